@@ -154,6 +154,88 @@ int sd_block_attn_append(const sd_attn_shape *shape, const void *q, const void *
                          size_t workspace_bytes, void *stream);
 
 /* ==========================================================================
+ * A prompt's way into a paged cache.  The speculative step starts from a cached context; these calls
+ * make it: norm and position rotation of a chunk's queries and keys, its keys and values into the
+ * pages, and the attention of the chunk over what is cached.  A prompt may come in any number of
+ * chunks, and chunks of prompts may share a batch with single tokens of other sequences.
+ * ========================================================================== */
+typedef struct sd_rope_shape {
+  int32_t num_seqs;     /* S >= 0 (sd_kv_append_rope_paged; else unused) */
+  int32_t total_q;      /* rows (tokens) >= 0 */
+  int32_t num_q_heads;  /* Hq >= 0 (0: no queries) */
+  int32_t num_kv_heads; /* Hkv >= 0 (0: no keys; at least 1 for sd_kv_append_rope_paged); any ratio to Hq */
+  int32_t head_dim;     /* D: 64 or 128 */
+  int32_t rot_dim;      /* R: dims that are rotated, a multiple of 16 in [0, D]; dims R .. D-1 pass */
+  int32_t interleaved;  /* pair i of a head is dims (i, R/2 + i) if 0, (2i, 2i + 1) if 1 */
+  int32_t dtype;        /* SD_BF16 or SD_F32: rows, norm weights, outputs and pages */
+  float eps;            /* added to the mean square, finite and >= 0 */
+  float rot_scale;      /* factor on cosines and sines (context extension); 0 means 1 */
+  /* elements from one token's row to the next, 0 for packed rows: at least heads * D, a multiple of 16
+     bytes, at most 2^32 */
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+} sd_rope_shape;
+
+/*
+ * Every head x of q and k: x^ = x / sqrt(mean_d(x_d^2) + eps) * weight (only where a weight is given),
+ * then pair i < R/2 (a, b) becomes (a c - b s, b c + a s) with c, s = rot_scale * cos, sin of
+ * positions[r] * inv_freq[i].  Angles are reduced in 64 bits, everything else is fp32, rounded to
+ * dtype once.
+ *   q, q_out     [total_q, Hq, D]   dtype, row strides q_stride, q_out_stride (both may be NULL if Hq == 0)
+ *   k, k_out     [total_q, Hkv, D]  dtype, row strides k_stride, k_out_stride (both may be NULL if Hkv == 0)
+ *   positions    [total_q] int32    any value
+ *   inv_freq     [R/2] fp32         (may be NULL if R == 0)
+ *   q_weight, k_weight [D] dtype    or NULL: no norm of q, of k
+ * An output may be its own input (same address and stride); otherwise outputs overlap nothing else.
+ * Host-checked preconditions: rows, weights and outputs 16-byte aligned; strides as in sd_rope_shape.
+ * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED (head_dim), SD_ERR_HIP.  total_q == 0 returns SD_OK
+ * without touching the device.
+ */
+int sd_qk_norm_rope(const sd_rope_shape *shape, const void *q, const void *k, const int32_t *positions,
+                    const float *inv_freq, const void *q_weight, const void *k_weight, void *q_out, void *k_out,
+                    void *stream);
+
+/*
+ * The same with row i of sequence s at position ctx_s + i, k written to logical key ctx_s + i of the
+ * page pools (laid out as in sd_block_attn_paged, dtype elements) and v copied there as it is.  q goes
+ * to q_out; without queries (Hq == 0) only keys and values are appended.
+ *   k_new, v_new     [total_q, Hkv, D]  dtype, row strides k_stride, v_stride
+ *   ctx_lens         [S] int32          committed length before the call
+ *   q_offsets        [S + 1] int32      exclusive prefix sum of the row counts, q_offsets[S] <= total_q
+ * Rows from q_offsets[S] on belong to no sequence: neither read into the pages nor written to q_out.
+ * A key or value past max_pages * page_size, or whose page id lies outside [0, num_pages), is skipped.
+ * page_size as in sd_block_attn_paged; max_pages * page_size < 2^31.  k_out_stride is not used.
+ * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED (head_dim), SD_ERR_HIP.
+ */
+int sd_kv_append_rope_paged(const sd_rope_shape *shape, int32_t page_size, int32_t num_pages, int32_t max_pages,
+                            const int32_t *block_table, const void *q, const void *k_new, const void *v_new,
+                            const int32_t *ctx_lens, const int32_t *q_offsets, const float *inv_freq,
+                            const void *q_weight, const void *k_weight, void *q_out, void *k_pages, void *v_pages,
+                            void *stream);
+
+/* Workspace bytes sd_chunk_attn_paged needs for this shape (host-only). */
+int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
+
+/*
+ * sd_block_attn_paged for any number of new rows per sequence: shape->max_block bounds chunk_lens.
+ * max_ctx and max_block lie in [0, max_kv_len] and [1, max_kv_len], and ctx_s + B_s <= max_kv_len for
+ * every s (their bounds' sum may be more); Hq/Hkv <= 256.
+ * Everything else is as there: bf16 page pools that already hold the chunk's keys and values, the masks,
+ * fp32 softmax and sums with weights rounded to bf16, asynchronous, no synchronisation.
+ *   chunk_lens [S] int32      rows of sequence s, 0 <= B_s <= max_block
+ *   q_offsets  [S + 1] int32  exclusive prefix sum of chunk_lens, q_offsets[S] <= total_q; rows of out
+ *                             from q_offsets[S] on are left as they were
+ * Keys and values of a sequence at [0, ctx_s + B_s) are finite: a value that is not reaches every row of the
+ * tile that holds it, masked for that row or not (0 * inf).  What lies behind ctx_s + B_s in a page is
+ * never read.
+ * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED (head_dim, group size, dtype), SD_ERR_WORKSPACE,
+ * SD_ERR_HIP.  S == 0 or total_q == 0 returns SD_OK without touching the device.
+ */
+int sd_chunk_attn_paged(const sd_attn_shape *shape, int32_t page_size, int32_t num_pages, int32_t max_pages,
+                        const int32_t *block_table, const void *q, const void *k_pages, const void *v_pages,
+                        const int32_t *ctx_lens, const int32_t *chunk_lens, const int32_t *q_offsets,
+                        int32_t mask_mode, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ==========================================================================
  * Speculative acceptance (Fig. 1 caption: accept the longest consistent prefix;
  * Sec. 1 and Sec. 3.1: the target's output distribution is preserved exactly).
  * Block layout: position 0 of a block is the last committed token (the anchor),

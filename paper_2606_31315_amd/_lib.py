@@ -22,7 +22,8 @@ EXPORTS = ["sd_last_error", "sd_version", "sd_block_attn_workspace_size", "sd_bl
            "sd_accept_workspace_size", "sd_accept", "sd_kv_append", "sd_commit", "sd_verify_step_workspace_size",
            "sd_verify_step", "sd_policy_workspace_size", "sd_block_size_policy", "sd_block_attn_paged",
            "sd_kv_append_paged", "sd_survival_tau", "sd_survival_sample", "sd_block_attn_append",
-           "sd_check_attn_inputs", "sd_check_accept_inputs", "sd_accept_noalloc", "sd_accept_set_path"]
+           "sd_check_attn_inputs", "sd_check_accept_inputs", "sd_accept_noalloc", "sd_accept_set_path",
+           "sd_qk_norm_rope", "sd_kv_append_rope_paged", "sd_chunk_attn_workspace_size", "sd_chunk_attn_paged"]
 
 # bytes of the fixed device scratch behind sd_accept_noalloc (SD_ACCEPT_NOALLOC_SCRATCH_BYTES)
 ACCEPT_NOALLOC_SCRATCH_BYTES = 4 << 20
@@ -50,6 +51,14 @@ class SdPolicyShape(ctypes.Structure):
 class SdSurvivalShape(ctypes.Structure):
     _fields_ = [("num_samples", ctypes.c_int32), ("max_pos", ctypes.c_int32), ("num_cands", ctypes.c_int32),
                 ("train_block", ctypes.c_int32), ("alpha", ctypes.c_double), ("cands", ctypes.c_int32 * 64)]
+
+
+class SdRopeShape(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("total_q", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("rot_scale", ctypes.c_float), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64)]
 
 
 class SdLayerBuffers(ctypes.Structure):
@@ -119,6 +128,14 @@ def lib() -> ctypes.CDLL:
         L.sd_accept_set_path.argtypes = [I, I]
         L.sd_check_accept_inputs.restype = ctypes.c_int
         L.sd_check_accept_inputs.argtypes = [ctypes.POINTER(SdAcceptShape), P, P, P, P, ctypes.c_float, P, P]
+        L.sd_qk_norm_rope.restype = ctypes.c_int
+        L.sd_qk_norm_rope.argtypes = [ctypes.POINTER(SdRopeShape), P, P, P, P, P, P, P, P, P]
+        L.sd_kv_append_rope_paged.restype = ctypes.c_int
+        L.sd_kv_append_rope_paged.argtypes = [ctypes.POINTER(SdRopeShape), I, I, I, P, P, P, P, P, P, P, P, P, P, P, P, P]
+        L.sd_chunk_attn_workspace_size.restype = ctypes.c_int
+        L.sd_chunk_attn_workspace_size.argtypes = [ctypes.POINTER(SdAttnShape), ctypes.POINTER(Z)]
+        L.sd_chunk_attn_paged.restype = ctypes.c_int
+        L.sd_chunk_attn_paged.argtypes = [ctypes.POINTER(SdAttnShape), I, I, I, P, P, P, P, P, P, P, I, P, P, Z, P]
         _lib = L
     return _lib
 
@@ -401,6 +418,159 @@ def kv_append_paged(k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Ten
     _check(lib().sd_kv_append_paged(ctypes.byref(shape), page_size, num_pages, max_pages, _ptr(block_table),
                                     _ptr(k_new), _ptr(v_new), _ptr(k_pages), _ptr(v_pages), _ptr(ctx_lens),
                                     _ptr(q_offsets), _stream(stream)))
+
+
+def _rows(t: Optional[torch.Tensor], name: str, dtype, dev, N, H, D) -> int:
+    """t must hold N token rows [N, H, D] whose heads lie side by side, the rows any stride of at least a
+    row apart (a slice of a packed projection).  Returns that stride in elements."""
+    _shape(t, name, N, H, D)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    N, H, D = t.shape
+    st = t.stride()
+    if st[2] != 1 or (H > 1 and st[1] != D) or (N > 1 and st[0] < H * D):
+        raise ValueError(f"{name} must hold rows of {H} heads of {D} elements side by side, got strides {list(st)}")
+    return st[0] if N > 1 else H * D
+
+
+def _norm_weight(w: Optional[torch.Tensor], name: str, like: torch.Tensor) -> None:
+    if w is not None:
+        _shape(w, name, like.shape[2])
+        _need(w, name, like.dtype, like.device)
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+                 inv_freq: Optional[torch.Tensor], *, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                 rot_scale: float = 0.0, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Norm of every head of q [N, Hq, D] and k [N, Hkv, D] (where a weight [D] is given) and their rotation by
+    positions [N] int32 in one pass (sd_qk_norm_rope).  Rows may be strided (slices of a packed
+    projection); inv_freq [R/2] fp32 rotates the first R dims (None: none).  q or k may be None; an output
+    may be its input.  Returns (q_out, k_out)."""
+    x = q if q is not None else k
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("q or k must be a torch.Tensor")
+    if x.dim() != 3:
+        raise ValueError(f"rows must have shape [N, heads, D], got {list(x.shape)}")
+    N, _, D = x.shape
+    dev, dt = x.device, x.dtype
+    _shape(positions, "positions", N)
+    _need(positions, "positions", torch.int32, dev)
+    if inv_freq is not None:
+        _shape(inv_freq, "inv_freq", None)
+        _need(inv_freq, "inv_freq", torch.float32, dev)
+    sh = SdRopeShape(0, N, 0, 0, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(bool(interleaved)),
+                     _dtype_code(x), float(eps), float(rot_scale))
+    if q is not None:
+        sh.q_stride, sh.num_q_heads = _rows(q, "q", dt, dev, N, None, D), q.shape[1]
+        _norm_weight(q_weight, "q_weight", q)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        sh.q_out_stride = _rows(q_out, "q_out", dt, dev, N, q.shape[1], D)
+    if k is not None:
+        sh.k_stride, sh.num_kv_heads = _rows(k, "k", dt, dev, N, None, D), k.shape[1]
+        _norm_weight(k_weight, "k_weight", k)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=dt, device=dev)
+        sh.k_out_stride = _rows(k_out, "k_out", dt, dev, N, k.shape[1], D)
+    if (q is None and (q_out is not None or q_weight is not None)) or (
+            k is None and (k_out is not None or k_weight is not None)):
+        raise ValueError("an output or a weight is given for rows that are not")
+    _check(lib().sd_qk_norm_rope(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq), _ptr(q_weight),
+                                 _ptr(k_weight), _ptr(q_out), _ptr(k_out), _stream(stream)))
+    return q_out, k_out
+
+
+def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor,
+                         v_pages: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                         q_offsets: torch.Tensor, inv_freq: Optional[torch.Tensor], *,
+                         q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                         eps: float = 1e-6, interleaved: bool = False, rot_scale: float = 0.0,
+                         q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """qk_norm_rope at positions ctx_s + i, with k and v written into page pools [num_pages, Hkv, page_size, D]
+    through block_table [S, max_pages] (sd_kv_append_rope_paged).  q may be None (append only).  Returns q_out."""
+    _shape(k_pages, "k_pages", None, None, None, None)
+    _shape(v_pages, "v_pages", *k_pages.shape)
+    num_pages, Hkv, page_size, D = k_pages.shape
+    dev, dt = k_pages.device, k_pages.dtype
+    _need(k_pages, "k_pages")
+    _need(v_pages, "v_pages", dt, dev)
+    ks = _rows(k_new, "k_new", dt, dev, None, Hkv, D)
+    N = k_new.shape[0]
+    vs = _rows(v_new, "v_new", dt, dev, N, Hkv, D)
+    _shape(block_table, "block_table", None, None)
+    S, max_pages = block_table.shape
+    _lens_shapes(S, ctx_lens=ctx_lens, q_offsets=q_offsets)
+    for name, t in (("block_table", block_table), ("ctx_lens", ctx_lens), ("q_offsets", q_offsets)):
+        _need(t, name, torch.int32, dev)
+    if inv_freq is not None:
+        _shape(inv_freq, "inv_freq", None)
+        _need(inv_freq, "inv_freq", torch.float32, dev)
+    _norm_weight(k_weight, "k_weight", k_new)
+    sh = SdRopeShape(S, N, 0, Hkv, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(bool(interleaved)),
+                     _dtype_code(k_pages), float(eps), float(rot_scale), 0, ks, vs)
+    if q is not None:
+        sh.q_stride, sh.num_q_heads = _rows(q, "q", dt, dev, N, None, D), q.shape[1]
+        _norm_weight(q_weight, "q_weight", q)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        sh.q_out_stride = _rows(q_out, "q_out", dt, dev, N, q.shape[1], D)
+    elif q_out is not None or q_weight is not None:
+        raise ValueError("an output or a weight is given for rows that are not")
+    _check(lib().sd_kv_append_rope_paged(ctypes.byref(sh), page_size, num_pages, max_pages, _ptr(block_table), _ptr(q),
+                                         _ptr(k_new), _ptr(v_new), _ptr(ctx_lens), _ptr(q_offsets), _ptr(inv_freq),
+                                         _ptr(q_weight), _ptr(k_weight), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
+                                         _stream(stream)))
+    return q_out
+
+
+def chunk_attn_workspace_size(shape: SdAttnShape) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().sd_chunk_attn_workspace_size(ctypes.byref(shape), ctypes.byref(n)))
+    return n.value
+
+
+def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,
+                     ctx_lens: torch.Tensor, chunk_lens: torch.Tensor, q_offsets: torch.Tensor, mask_mode: int, *,
+                     max_ctx: int, max_chunk: int, scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
+    without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths."""
+    _shape(k_pages, "k_pages", None, None, None, None)
+    _shape(v_pages, "v_pages", *k_pages.shape)
+    _shape(q, "q", None, None, k_pages.shape[3])
+    _shape(block_table, "block_table", None, None)
+    _lens_shapes(block_table.shape[0], ctx_lens=ctx_lens, chunk_lens=chunk_lens, q_offsets=q_offsets)
+    if out is not None:
+        _shape(out, "out", *q.shape)
+    dev = q.device
+    for name, t in (("q", q), ("k_pages", k_pages), ("v_pages", v_pages)):
+        _need(t, name, torch.bfloat16, dev)
+    for name, t in (("block_table", block_table), ("ctx_lens", ctx_lens), ("chunk_lens", chunk_lens),
+                    ("q_offsets", q_offsets)):
+        _need(t, name, torch.int32, dev)
+    num_pages, Hkv, page_size, D = k_pages.shape
+    S, max_pages = block_table.shape
+    if out is None:
+        out = torch.empty_like(q)
+    _need(out, "out", q.dtype, dev)
+    total_q, Hq, _ = q.shape
+    key = ("chunk", S, Hq, Hkv, D, max_pages, page_size, total_q, int(max_ctx), int(max_chunk), float(scale))
+    _, ref, nbytes = _cached_call(key, lambda: SdAttnShape(S, Hq, Hkv, D, max_pages * page_size, total_q, int(max_ctx),
+                                                           int(max_chunk), SD_BF16, float(scale)),
+                                  chunk_attn_workspace_size)
+    if workspace is None:
+        workspace = _default_ws.get(nbytes, dev)
+    _check(lib().sd_chunk_attn_paged(ref, page_size, num_pages, max_pages, _ptr(block_table), _ptr(q), _ptr(k_pages),
+                                     _ptr(v_pages), _ptr(ctx_lens), _ptr(chunk_lens), _ptr(q_offsets), int(mask_mode),
+                                     _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                     _stream(stream)))
+    return out
 
 
 def accept_shape(target_logits: torch.Tensor, num_seqs: int, max_block: int) -> SdAcceptShape:

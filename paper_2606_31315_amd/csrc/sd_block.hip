@@ -1,7 +1,7 @@
 // sd_block.hip -- C ABI of libsdblock.so (declared in include/sd_block.h).
 //
 // Host side only: argument validation, workspace layout, launch planning and kernel
-// dispatch.  The arithmetic lives in attn.hpp and accept.hpp.
+// dispatch.  The arithmetic lives in the kernels' headers.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdarg.h>
@@ -19,8 +19,10 @@
 #include "attn_bf16.hpp"
 #include "attn_f32.hpp"
 #include "check.hpp"
+#include "chunk.hpp"
 #include "kvstep.hpp"
 #include "policy.hpp"
+#include "rope.hpp"
 #include "sd_block.h"
 #include "survival.hpp"
 
@@ -423,6 +425,20 @@ int policy_plan(const sd_policy_shape *sh, PolicyPlan *p) {
   return ok();
 }
 
+template <bool PAGED>
+void launch_rope(const sd_rope_shape *sh, const sdb::RopeArgs &a, hipStream_t st) {
+  const long long blocks = ((long long)a.total_q * a.groups + 3) / 4;
+  const dim3 grid((unsigned)std::min(blocks, 1LL << 20)), block(256);
+  const bool bf16 = sh->dtype == SD_BF16;
+  if (sh->head_dim == 128) {
+    if (bf16) hipLaunchKernelGGL((sdb::rope_kernel<true, 128, PAGED>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((sdb::rope_kernel<false, 128, PAGED>), grid, block, 0, st, a);
+  } else {
+    if (bf16) hipLaunchKernelGGL((sdb::rope_kernel<true, 64, PAGED>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((sdb::rope_kernel<false, 64, PAGED>), grid, block, 0, st, a);
+  }
+}
+
 template <bool RELU, int XM>
 void launch_dense(const sdb::DenseArgs &d, hipStream_t st) {
   const dim3 grid((d.rows + sdb::kDenseRows - 1) / sdb::kDenseRows);
@@ -660,6 +676,219 @@ int sd_kv_append_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_p
   a.num_pages = num_pages;
   hipLaunchKernelGGL(sdb::kv_append_paged_kernel, dim3(sh->total_q, 2), dim3(256), 0, (hipStream_t)stream, a);
   return check_launch("sd_kv_append_paged");
+}
+
+// ---------------------------------------------------------------------------
+// attention of chunks over page pools
+// ---------------------------------------------------------------------------
+namespace {
+
+struct ChunkPlan {
+  bool block;             // small blocks: the block attention's kernels
+  sd_attn_shape block_sh; // their shape
+  size_t total;   // workspace bytes
+};
+
+int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
+  int rc = check_cache_shape(sh, "sd_chunk_attn_paged");
+  if (rc) return rc;
+  if (sh->dtype != SD_BF16) return fail(SD_ERR_UNSUPPORTED, "paged caches are bf16 only");
+  if (sh->max_ctx < 0 || sh->max_ctx > sh->max_kv_len)
+    return fail(SD_ERR_INVALID_ARG, "max_ctx must be in [0, max_kv_len] (got %d)", sh->max_ctx);
+  if (sh->max_block < 1 || sh->max_block > sh->max_kv_len)
+    return fail(SD_ERR_INVALID_ARG, "max_block must be in [1, max_kv_len] (got %d)", sh->max_block);
+  if ((long long)sh->total_q > (long long)sh->num_seqs * sh->max_block)
+    return fail(SD_ERR_INVALID_ARG, "total_q %d outside [0, num_seqs * max_block]", sh->total_q);
+  const int G = sh->num_q_heads / sh->num_kv_heads;
+  if (G > sdb::kChunkRows) return fail(SD_ERR_UNSUPPORTED, "group size %d exceeds %d", G, sdb::kChunkRows);
+  if (!(sh->scale >= 0.f) || isinf(sh->scale)) return fail(SD_ERR_INVALID_ARG, "scale must be finite and >= 0");
+  const int P = sdb::kChunkRows / G;
+  if (((long long)sh->total_q / P + sh->num_seqs) * sh->num_kv_heads >= 1LL << 24)
+    return fail(SD_ERR_INVALID_ARG, "problem too large");
+  p->block = sh->max_block <= 64 && G * sh->max_block <= 256;
+  p->total = 256;
+  if (p->block) {
+    // They are planned for the longest ctx_s + B_s, max_ctx + max_block; here max_kv_len bounds it too.
+    p->block_sh = *sh;
+    p->block_sh.max_ctx = std::min(sh->max_ctx, sh->max_kv_len - sh->max_block);
+    AttnPlan ap;
+    rc = attn_plan(&p->block_sh, &ap);
+    if (rc) return rc;
+    p->total = ap.total;
+  }
+  return ok();
+}
+
+}  // namespace
+
+int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes) {
+  if (!bytes) return fail(SD_ERR_INVALID_ARG, "bytes is NULL");
+  ChunkPlan p;
+  int rc = chunk_plan(shape, &p);
+  if (rc) return rc;
+  *bytes = p.total;
+  return ok();
+}
+
+int sd_chunk_attn_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_pages, int32_t max_pages,
+                        const int32_t *block_table, const void *q, const void *k_pages, const void *v_pages,
+                        const int32_t *ctx_lens, const int32_t *chunk_lens, const int32_t *q_offsets,
+                        int32_t mask_mode, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  ChunkPlan p;
+  int rc = chunk_plan(sh, &p);
+  if (rc) return rc;
+  int log2 = 0;
+  rc = check_pages(sh, page_size, num_pages, max_pages, &log2);
+  if (rc) return rc;
+  if (mask_mode != SD_MASK_CAUSAL_IN_BLOCK && mask_mode != SD_MASK_BIDIR_IN_BLOCK)
+    return fail(SD_ERR_INVALID_ARG, "unknown mask_mode %d", mask_mode);
+  if (sh->num_seqs == 0 || sh->total_q == 0) return ok();
+  if (!block_table || !q || !k_pages || !v_pages || !out || !ctx_lens || !chunk_lens || !q_offsets || !workspace)
+    return fail(SD_ERR_INVALID_ARG, "sd_chunk_attn_paged: NULL pointer argument");
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out))
+    return fail(SD_ERR_INVALID_ARG, "q, page pools and out must be 16-byte aligned");
+  if (((uintptr_t)workspace & 255u) != 0) return fail(SD_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (workspace_bytes < p.total)
+    return fail(SD_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, p.total);
+  if (p.block)
+    return sd_block_attn_paged(&p.block_sh, page_size, num_pages, max_pages, block_table, q, k_pages, v_pages, ctx_lens,
+                               chunk_lens, q_offsets, mask_mode, out, workspace, workspace_bytes, stream);
+  sdb::ChunkArgs a;
+  a.q = q;
+  a.k = k_pages;
+  a.v = v_pages;
+  a.out = out;
+  a.ctx_lens = ctx_lens;
+  a.chunk_lens = chunk_lens;
+  a.q_offsets = q_offsets;
+  a.block_table = block_table;
+  a.S = sh->num_seqs;
+  a.Hq = sh->num_q_heads;
+  a.Hkv = sh->num_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.P = sdb::kChunkRows / a.G;
+  a.page_log2 = log2;
+  a.max_pages = max_pages;
+  a.num_pages = num_pages;
+  a.causal = mask_mode == SD_MASK_CAUSAL_IN_BLOCK;
+  const float scale = sh->scale > 0.f ? sh->scale : 1.0f / sqrtf((float)sh->head_dim);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const unsigned grid = (unsigned)((sh->total_q / a.P + sh->num_seqs) * sh->num_kv_heads);
+  if (sh->head_dim == 128) hipLaunchKernelGGL(sdb::chunk_attn_kernel<128>, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(sdb::chunk_attn_kernel<64>, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
+  return check_launch("sd_chunk_attn_paged");
+}
+
+// ---------------------------------------------------------------------------
+// norm and rotation of queries and keys, with or without the append to page pools
+// ---------------------------------------------------------------------------
+namespace {
+
+// Stride in elements between a tensor's rows of `heads` heads (0: packed): at least a row, so no two
+// rows share elements, and whole 16-byte vectors.
+int rope_stride(const sd_rope_shape *sh, const char *name, int64_t stride, int heads, long long *out) {
+  const int64_t row = (int64_t)heads * sh->head_dim;
+  if (stride == 0) stride = row;
+  if (stride < row) return fail(SD_ERR_INVALID_ARG, "%s %lld is less than a row (%lld elements)", name, (long long)stride, (long long)row);
+  if (stride > (1LL << 32)) return fail(SD_ERR_INVALID_ARG, "%s %lld is too large", name, (long long)stride);
+  if (stride % (sh->dtype == SD_BF16 ? 8 : 4))
+    return fail(SD_ERR_INVALID_ARG, "%s %lld is not a multiple of 16 bytes", name, (long long)stride);
+  *out = stride;
+  return SD_OK;
+}
+
+int rope_args(const sd_rope_shape *sh, bool paged, const char *what, const void *q, const void *k, const void *v,
+              const float *inv_freq, const void *qw, const void *kw, void *q_out, void *k_out, sdb::RopeArgs *a) {
+  if (!sh) return fail(SD_ERR_INVALID_ARG, "%s: shape is NULL", what);
+  if (sh->num_seqs < 0 || sh->total_q < 0)
+    return fail(SD_ERR_INVALID_ARG, "num_seqs and total_q must be >= 0 (got %d, %d)", sh->num_seqs, sh->total_q);
+  if (sh->num_q_heads < 0 || sh->num_kv_heads < (paged ? 1 : 0) || sh->num_q_heads > 65536 || sh->num_kv_heads > 65536 ||
+      sh->num_q_heads + sh->num_kv_heads < 1)
+    return fail(SD_ERR_INVALID_ARG, "%s: head counts out of range (Hq=%d, Hkv=%d)", what, sh->num_q_heads, sh->num_kv_heads);
+  if (sh->dtype != SD_BF16 && sh->dtype != SD_F32) return fail(SD_ERR_INVALID_ARG, "unknown dtype %d", sh->dtype);
+  if (sh->head_dim != 64 && sh->head_dim != 128)
+    return fail(SD_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", sh->head_dim);
+  if (sh->rot_dim < 0 || sh->rot_dim > sh->head_dim || sh->rot_dim % 16)
+    return fail(SD_ERR_INVALID_ARG, "rot_dim must be a multiple of 16 in [0, head_dim] (got %d)", sh->rot_dim);
+  if (sh->interleaved != 0 && sh->interleaved != 1)
+    return fail(SD_ERR_INVALID_ARG, "interleaved must be 0 or 1 (got %d)", sh->interleaved);
+  if (!(sh->eps >= 0.f) || isinf(sh->eps)) return fail(SD_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (!isfinite(sh->rot_scale)) return fail(SD_ERR_INVALID_ARG, "rot_scale must be finite");
+  *a = sdb::RopeArgs{};
+  int rc = rope_stride(sh, "q_stride", sh->q_stride, sh->num_q_heads, &a->q_stride);
+  if (!rc) rc = rope_stride(sh, "k_stride", sh->k_stride, sh->num_kv_heads, &a->k_stride);
+  if (!rc) rc = rope_stride(sh, "q_out_stride", sh->q_out_stride, sh->num_q_heads, &a->q_out_stride);
+  if (!rc && paged) rc = rope_stride(sh, "v_stride", sh->v_stride, sh->num_kv_heads, &a->v_stride);
+  if (!rc && !paged) rc = rope_stride(sh, "k_out_stride", sh->k_out_stride, sh->num_kv_heads, &a->k_out_stride);
+  if (rc) return rc;
+  if (sh->total_q > 0 && (!paged || sh->num_seqs > 0)) {
+    if ((sh->num_q_heads && (!q || !q_out)) || (sh->num_kv_heads && (!k || (paged ? !v : !k_out))) || (sh->rot_dim && !inv_freq))
+      return fail(SD_ERR_INVALID_ARG, "%s: NULL pointer argument", what);
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(qw) || !aligned16(kw))
+      return fail(SD_ERR_INVALID_ARG, "rows, norm weights and outputs must be 16-byte aligned");
+  }
+  a->q = q;
+  a->k = k;
+  a->v = v;
+  a->q_out = q_out;
+  a->k_out = k_out;
+  a->inv_freq = inv_freq;
+  a->qw = qw;
+  a->kw = kw;
+  a->total_q = sh->total_q;
+  a->Hq = sh->num_q_heads;
+  a->Hkv = sh->num_kv_heads;
+  a->rot = sh->rot_dim;
+  a->interleaved = sh->interleaved;
+  a->eps = sh->eps;
+  a->rot_scale = sh->rot_scale == 0.f ? 1.f : sh->rot_scale;
+  const int hpw = 1024 / sh->head_dim;  // heads a wavefront takes
+  a->groups = (sh->num_q_heads + (paged ? 2 : 1) * sh->num_kv_heads + hpw - 1) / hpw;
+  return ok();
+}
+
+}  // namespace
+
+int sd_qk_norm_rope(const sd_rope_shape *sh, const void *q, const void *k, const int32_t *positions,
+                    const float *inv_freq, const void *q_weight, const void *k_weight, void *q_out, void *k_out,
+                    void *stream) {
+  sdb::RopeArgs a;
+  int rc = rope_args(sh, false, "sd_qk_norm_rope", q, k, nullptr, inv_freq, q_weight, k_weight, q_out, k_out, &a);
+  if (rc) return rc;
+  if (sh->total_q == 0) return ok();
+  if (!positions) return fail(SD_ERR_INVALID_ARG, "sd_qk_norm_rope: NULL pointer argument");
+  a.positions = positions;
+  launch_rope<false>(sh, a, (hipStream_t)stream);
+  return check_launch("sd_qk_norm_rope");
+}
+
+int sd_kv_append_rope_paged(const sd_rope_shape *sh, int32_t page_size, int32_t num_pages, int32_t max_pages,
+                            const int32_t *block_table, const void *q, const void *k_new, const void *v_new,
+                            const int32_t *ctx_lens, const int32_t *q_offsets, const float *inv_freq,
+                            const void *q_weight, const void *k_weight, void *q_out, void *k_pages, void *v_pages,
+                            void *stream) {
+  sdb::RopeArgs a;
+  int rc = rope_args(sh, true, "sd_kv_append_rope_paged", q, k_new, v_new, inv_freq, q_weight, k_weight, q_out, nullptr, &a);
+  if (rc) return rc;
+  int log2 = 0;
+  rc = check_pages(nullptr, page_size, num_pages, max_pages, &log2);
+  if (rc) return rc;
+  if ((long long)max_pages * page_size > INT32_MAX) return fail(SD_ERR_INVALID_ARG, "max_pages * page_size exceeds 2^31 - 1");
+  if (sh->num_seqs == 0 || sh->total_q == 0) return ok();
+  if (!block_table || !ctx_lens || !q_offsets || !k_pages || !v_pages)
+    return fail(SD_ERR_INVALID_ARG, "sd_kv_append_rope_paged: NULL pointer argument");
+  if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(SD_ERR_INVALID_ARG, "page pools must be 16-byte aligned");
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.ctx_lens = ctx_lens;
+  a.q_offsets = q_offsets;
+  a.block_table = block_table;
+  a.S = sh->num_seqs;
+  a.page_log2 = log2;
+  a.max_pages = max_pages;
+  a.num_pages = num_pages;
+  launch_rope<true>(sh, a, (hipStream_t)stream);
+  return check_launch("sd_kv_append_rope_paged");
 }
 
 int sd_accept_workspace_size(const sd_accept_shape *shape, float temperature, size_t *bytes) {

@@ -1,0 +1,189 @@
+"""sd_chunk_attn_paged against the plain form in 64 bits: ragged chunks from no row to hundreds, head
+groups, head sizes, pages that end inside a tile, both masks; what must not change does not."""
+import numpy as np
+import pytest
+import torch
+
+import gpu_util as G
+import paper_2606_31315_amd as sd
+import prefill_ref as R
+
+pytestmark = pytest.mark.gpu
+CAUSAL, BIDIR = R.CAUSAL, R.BIDIR
+
+
+def _i32(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(G.dev())
+
+
+def _run(b, mask, **kw):
+    kw.setdefault("max_ctx", int(b["ctx"].max()))
+    kw.setdefault("max_chunk", max(1, int(b["B"].max())))
+    G.log(f"sd_chunk_attn_paged q={list(b['q'].shape)} pool={list(b['kp'].shape)} ctx={b['ctx'][:8].tolist()} "
+          f"B={b['B'][:8].tolist()} mask={mask}")
+    o = sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], _i32(b["ctx"]), _i32(b["B"]), _i32(b["off"]), mask, **kw)
+    torch.cuda.synchronize()
+    return o
+
+
+def _check(b, mask, scale=0.0, **kw):
+    o = _run(b, mask, scale=scale, **kw)
+    R.assert_attended(o, b["q"], b["kp"], b["vp"], b["table"], b["ctx"], b["B"], b["off"], mask, scale)
+    return o
+
+
+CASES = [  # Hq, Hkv, D, page, contexts, rows
+    ("one_row_over_64", 32, 8, 128, 16, [0], [65]),
+    ("tile_edges", 32, 8, 128, 64, [0, 64, 63, 1], [64, 65, 128, 63]),
+    ("odd_lengths", 32, 8, 128, 16, [1000, 17, 0, 333], [131, 77, 5, 200]),
+    ("rows_of_every_kind", 32, 8, 128, 32, [500, 0, 2000, 129, 0, 64], [1, 0, 300, 1, 1, 64]),
+    ("one_head_to_a_group", 8, 8, 128, 64, [100, 0], [300, 257]),
+    ("all_heads_in_a_group", 32, 1, 128, 256, [777, 5], [70, 9]),
+    ("group_of_five", 10, 2, 128, 16, [90, 0], [140, 66]),
+    ("group_of_eight_small_heads", 32, 4, 64, 128, [1500, 3], [90, 100]),
+    ("small_heads", 8, 8, 64, 32, [300, 0, 47], [260, 512, 1]),
+    ("group_of_three_small_heads", 6, 2, 64, 16, [10, 700], [170, 86]),
+    ("long_context_few_rows", 32, 8, 128, 64, [9000], [70]),
+    ("single_rows_beside_a_chunk", 32, 8, 128, 16, [3000, 1999, 12, 700, 1], [1, 1, 1, 400, 1]),
+]
+
+
+@pytest.mark.parametrize("mask", [CAUSAL, BIDIR], ids=["causal", "bidir"])
+@pytest.mark.parametrize("name,Hq,Hkv,D,page,ctx,B", CASES, ids=[c[0] for c in CASES])
+def test_parity(name, Hq, Hkv, D, page, ctx, B, mask):
+    _check(R.chunk_batch(len(name), Hq, Hkv, D, page, ctx, B, G.dev()), mask)
+
+
+@pytest.mark.parametrize("B", [[1, 1, 1], [5, 16, 0], [17, 64, 33]], ids=["tokens", "blocks", "to_64_rows"])
+def test_short_chunks(B):
+    """Batches that the block attention's kernels take."""
+    _check(R.chunk_batch(11, 32, 8, 128, 32, [700, 0, 2500], B, G.dev()), CAUSAL)
+
+
+def test_many_sequences():
+    """More than 64 sequences: the lookup of a workgroup's share crosses rounds, with empty ones at its edge."""
+    rng = np.random.default_rng(5)
+    B = rng.integers(0, 90, 150)
+    B[[0, 62, 63, 64, 127, 128, 149]] = [0, 0, 0, 81, 0, 3, 0]
+    _check(R.chunk_batch(6, 16, 8, 64, 16, rng.integers(0, 300, 150), B, G.dev()), CAUSAL)
+
+
+@pytest.mark.parametrize("sigma,scale", [(6.0, 0.0), (1.0, 0.5), (1e-3, 0.0)], ids=["sharp", "scaled", "flat"])
+def test_scores(sigma, scale):
+    """Sharp and flat softmaxes, a scale of the caller's: the running maximum moves often, or not."""
+    _check(R.chunk_batch(21, 16, 4, 128, 64, [600, 50], [130, 200], G.dev(), sigma=sigma), CAUSAL, scale=scale)
+
+
+def test_growing_scores():
+    """Keys whose scores grow along the context, by far more than any threshold at once: every step moves the
+    maximum."""
+    b = R.chunk_batch(22, 8, 2, 128, 64, [700], [100], G.dev())
+    b["q"].copy_(b["q"].abs())
+    for s in range(1):
+        n = b["table"].shape[1]
+        ramp = (torch.arange(n * 64, device=G.dev()) / 100.0).reshape(1, n, 64, 1).transpose(0, 1)
+        b["kp"][b["table"][s].long()] = (b["kp"][b["table"][s].long()] * 0.05 + ramp).to(torch.bfloat16)
+    _check(b, CAUSAL, scale=0.05)
+
+
+def test_loose_bounds_and_padding():
+    """Bounds far above the lengths, a batch padded with rows and sequences: rows behind the last sequence
+    stay as they were."""
+    b = R.chunk_batch(31, 32, 8, 128, 16, [300, 0, 40, 0], [100, 0, 71, 0], G.dev())
+    n = int(b["off"][-1])
+    b["q"] = torch.cat([b["q"], torch.full((37, 32, 128), float("nan"), dtype=torch.bfloat16, device=G.dev())])
+    table = torch.zeros(4, 1024, dtype=torch.int32, device=G.dev())
+    table[:, :b["table"].shape[1]] = b["table"]
+    b["table"] = table
+    out = torch.full_like(b["q"], 7.0)
+    o = _check(b, CAUSAL, out=out, max_ctx=9000, max_chunk=5000)
+    assert o is out and bool((out[n:] == 7.0).all())
+
+
+def test_minus_infinite_and_lowest_scores():
+    """A key that nothing may weigh (score of the type's lowest values, -inf): weight 0, as in softmax."""
+    b = R.chunk_batch(41, 4, 4, 128, 64, [200], [80], G.dev())
+    b["q"].copy_(b["q"].abs() + 0.5)
+    t = b["table"][0].long()
+    b["kp"][t[0], :, 5] = -torch.finfo(torch.bfloat16).max / 1024
+    b["kp"][t[1], :, 3] = float("-inf")
+    _check(b, CAUSAL)
+
+
+def test_page_ids_outside_the_pool_stay_inside():
+    """Ids that the contract forbids are clamped into the pool: sequences with sound ids are not touched by it."""
+    b = R.chunk_batch(51, 16, 8, 128, 16, [100, 90], [70, 80], G.dev())
+    good = _run(b, CAUSAL)
+    b["table"] = b["table"].clone()
+    b["table"][0, 1], b["table"][0, 2] = 2 ** 30, -5
+    bad = _run(b, CAUSAL)
+    assert torch.equal(bad[70:], good[70:])
+
+
+def test_pools_past_32_bit_offsets():
+    """Pages beyond 2^31 elements of the pool, the last one among them."""
+    dev, page, Hkv, D = G.dev(), 256, 8, 128
+    n = (1 << 31) // (Hkv * page * D) + 40
+    b = R.chunk_batch(61, 16, Hkv, D, page, [700], [100], dev)
+    kp, vp = (torch.empty((n, Hkv, page, D), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    ids = torch.tensor([n - 1, n - 30, 3, n - 2], device=dev)[:b["table"].shape[1]]
+    for big, x in ((kp, b["kp"]), (vp, b["vp"])):
+        big[ids] = x[b["table"][0].long()]
+    b.update(kp=kp, vp=vp, table=ids.to(torch.int32)[None].contiguous())
+    _check(b, CAUSAL)
+
+
+def test_same_call_same_bits_on_another_stream_and_workspace():
+    b = R.chunk_batch(71, 32, 8, 128, 64, [3000, 0, 511], [200, 333, 1], G.dev())
+    ref = _run(b, CAUSAL)
+    sh = sd._lib.SdAttnShape(3, 32, 8, 128, b["table"].shape[1] * 64, b["q"].shape[0], 3000, 333, sd.SD_BF16, 0.0)
+    ws = torch.full((sd.chunk_attn_workspace_size(sh),), 255, dtype=torch.uint8, device=G.dev())  # NaN throughout
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        got = _run(b, CAUSAL, workspace=ws)
+    assert torch.equal(got, ref)
+    assert torch.equal(_run(b, CAUSAL, stream=st), ref)
+
+
+@pytest.mark.parametrize("max_chunk", [64, 400], ids=["block_kernels", "chunk_kernel"])
+def test_graph_replays(max_chunk):
+    """Captured once, replayed with other lengths and contents inside the bounds: equal to eager calls."""
+    dev = G.dev()
+    b = R.chunk_batch(81, 16, 8, 128, 32, [2000, 1500, 64], [64 if max_chunk == 64 else 300, 20, 1], dev)
+    lens = [(b["ctx"], b["B"]), (b["ctx"] // 3, np.minimum(b["B"], [40, 20, 1])), (b["ctx"] * 0 + 5, b["B"] * 0 + 1)]
+    ctx, B, off = _i32(b["ctx"]), _i32(b["B"]), _i32(b["off"])
+    outs = {x: torch.zeros_like(b["q"]) for x in ("graph", "eager")}
+    sh = sd._lib.SdAttnShape(3, 16, 8, 128, b["table"].shape[1] * 32, b["q"].shape[0], 2000, max_chunk, sd.SD_BF16, 0.0)
+    ws = {x: torch.empty(sd.chunk_attn_workspace_size(sh), dtype=torch.uint8, device=dev) for x in outs}
+
+    def call(x):
+        sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], ctx, B, off, CAUSAL, max_ctx=2000,
+                            max_chunk=max_chunk, out=outs[x], workspace=ws[x])
+
+    call("eager")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call("graph")
+    for i in range(6):
+        c, n = lens[i % 3]
+        o = np.concatenate([[0], np.cumsum(n)])
+        ctx.copy_(_i32(c)), B.copy_(_i32(n)), off.copy_(_i32(o))
+        outs["graph"].zero_(), outs["eager"].zero_()
+        call("eager")
+        torch.cuda.synchronize()
+        G.log(f"  replay {i}")
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs["graph"], outs["eager"]), i
+
+
+def test_empty_calls():
+    dev = G.dev()
+    b = R.chunk_batch(91, 16, 8, 128, 16, [10, 0], [0, 0], dev)
+    assert _run(b, CAUSAL, max_chunk=16).shape[0] == 0
+    b = R.chunk_batch(92, 16, 8, 128, 16, [10], [80], dev)  # rows, but every sequence empty on the device
+    out = torch.full_like(b["q"], 3.0)
+    b["B"], b["off"] = b["B"] * 0, b["off"] * 0
+    assert bool((_run(b, CAUSAL, out=out, max_chunk=80) == 3.0).all())

@@ -1,0 +1,171 @@
+"""What the calls that put a prompt into a paged cache refuse, on the host before any device access: the C
+entry points by status code, the binding by exception."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2606_31315_amd import _lib as L
+
+P = ctypes.c_void_p
+
+
+def rope_shape(**kw):
+    sh = L.SdRopeShape(2, 20, 32, 8, 128, 128, 0, L.SD_BF16, 1e-6, 0.0, 0, 0, 0, 0, 0)
+    for k, v in kw.items():
+        setattr(sh, k, v)
+    return sh
+
+
+def rope(sh, **kw):
+    p = dict(q=4096, k=8192, pos=16, f=32, qw=4096, kw=4096, qo=12288, ko=16384)
+    p.update(kw)
+    return L.lib().sd_qk_norm_rope(ctypes.byref(sh) if sh is not None else None,
+                                   *(P(p[x]) for x in ("q", "k", "pos", "f", "qw", "kw", "qo", "ko")), None)
+
+
+def append(sh, page=16, pages=10, most=4, **kw):
+    p = dict(table=16, q=4096, k=8192, v=8192, ctx=16, off=16, f=32, qw=4096, kw=4096, qo=12288, kp=16384, vp=20480)
+    p.update(kw)
+    return L.lib().sd_kv_append_rope_paged(ctypes.byref(sh) if sh is not None else None, page, pages, most, *(
+        P(p[x]) for x in ("table", "q", "k", "v", "ctx", "off", "f", "qw", "kw", "qo", "kp", "vp")), None)
+
+
+@pytest.mark.parametrize("call", [rope, append])
+@pytest.mark.parametrize("field,value,code", [
+    ("total_q", -1, L.SD_ERR_INVALID_ARG), ("num_seqs", -1, L.SD_ERR_INVALID_ARG),
+    ("num_q_heads", -1, L.SD_ERR_INVALID_ARG), ("num_kv_heads", -1, L.SD_ERR_INVALID_ARG),
+    ("num_q_heads", 65537, L.SD_ERR_INVALID_ARG), ("head_dim", 96, L.SD_ERR_UNSUPPORTED),
+    ("rot_dim", -16, L.SD_ERR_INVALID_ARG), ("rot_dim", 24, L.SD_ERR_INVALID_ARG),
+    ("rot_dim", 144, L.SD_ERR_INVALID_ARG), ("interleaved", 2, L.SD_ERR_INVALID_ARG),
+    ("dtype", 2, L.SD_ERR_INVALID_ARG), ("eps", -1.0, L.SD_ERR_INVALID_ARG),
+    ("eps", float("nan"), L.SD_ERR_INVALID_ARG), ("eps", float("inf"), L.SD_ERR_INVALID_ARG),
+    ("rot_scale", float("inf"), L.SD_ERR_INVALID_ARG), ("rot_scale", float("nan"), L.SD_ERR_INVALID_ARG),
+    ("q_stride", 4088, L.SD_ERR_INVALID_ARG), ("q_stride", -4096, L.SD_ERR_INVALID_ARG),
+    ("q_stride", 4100, L.SD_ERR_INVALID_ARG), ("k_stride", 1000, L.SD_ERR_INVALID_ARG),
+    ("q_out_stride", 64, L.SD_ERR_INVALID_ARG), ("q_stride", (1 << 32) + 8, L.SD_ERR_INVALID_ARG),
+])
+def test_shape_errors(call, field, value, code):
+    assert call(rope_shape(**{field: value})) == code
+    assert L.lib().sd_last_error().decode()
+
+
+def test_rope_pointer_errors():
+    assert rope(None) == L.SD_ERR_INVALID_ARG
+    for x in ("q", "k", "pos", "f", "qo", "ko"):
+        assert rope(rope_shape(), **{x: None}) == L.SD_ERR_INVALID_ARG, x
+    for x in ("q", "k", "qo", "ko", "qw", "kw"):
+        assert rope(rope_shape(), **{x: 4104}) == L.SD_ERR_INVALID_ARG, x
+    assert rope(rope_shape(num_q_heads=0, num_kv_heads=0)) == L.SD_ERR_INVALID_ARG
+    assert rope(rope_shape(k_out_stride=8)) == L.SD_ERR_INVALID_ARG
+    assert rope(rope_shape(total_q=0), q=None, k=None, pos=None) == L.SD_OK
+
+
+def test_append_errors():
+    assert append(None) == L.SD_ERR_INVALID_ARG
+    for x in ("table", "q", "k", "v", "ctx", "off", "f", "qo", "kp", "vp"):
+        assert append(rope_shape(), **{x: None}) == L.SD_ERR_INVALID_ARG, x
+    for x in ("q", "k", "v", "qo", "kp", "vp", "qw", "kw"):
+        assert append(rope_shape(), **{x: 4104}) == L.SD_ERR_INVALID_ARG, x
+    for kw in (dict(page=8), dict(page=24), dict(page=8192), dict(pages=0), dict(most=0), dict(page=4096, most=1 << 20)):
+        assert append(rope_shape(), **kw) == L.SD_ERR_INVALID_ARG, kw
+    assert append(rope_shape(num_kv_heads=0)) == L.SD_ERR_INVALID_ARG
+    assert append(rope_shape(v_stride=512)) == L.SD_ERR_INVALID_ARG
+    assert append(rope_shape(num_seqs=0)) == L.SD_OK
+    assert append(rope_shape(total_q=0), q=None) == L.SD_OK
+
+
+def chunk_shape(**kw):
+    sh = L.SdAttnShape(4, 32, 8, 128, 4096, 900, 3000, 1000, L.SD_BF16, 0.0)
+    for k, v in kw.items():
+        setattr(sh, k, v)
+    return sh
+
+
+def chunk_ws(sh):
+    n = ctypes.c_size_t(0)
+    return L.lib().sd_chunk_attn_workspace_size(ctypes.byref(sh) if sh is not None else None, ctypes.byref(n)), n.value
+
+
+def chunk(sh, page=16, pages=10, most=256, mask=0, ws_bytes=None, ws=256, **kw):
+    p = dict(table=16, q=4096, k=8192, v=8192, ctx=16, len=16, off=16, out=12288)
+    p.update(kw)
+    n = chunk_ws(sh)[1] if ws_bytes is None else ws_bytes
+    return L.lib().sd_chunk_attn_paged(ctypes.byref(sh) if sh is not None else None, page, pages, most, *(
+        P(p[x]) for x in ("table", "q", "k", "v", "ctx", "len", "off")), mask, P(p["out"]), P(ws), n, None)
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("num_seqs", -1, L.SD_ERR_INVALID_ARG), ("num_q_heads", 0, L.SD_ERR_INVALID_ARG),
+    ("num_kv_heads", 5, L.SD_ERR_INVALID_ARG), ("head_dim", 96, L.SD_ERR_UNSUPPORTED),
+    ("max_block", 0, L.SD_ERR_INVALID_ARG), ("max_block", 4097, L.SD_ERR_INVALID_ARG), ("max_ctx", 4097, L.SD_ERR_INVALID_ARG),
+    ("max_ctx", -1, L.SD_ERR_INVALID_ARG), ("total_q", 4001, L.SD_ERR_INVALID_ARG),
+    ("total_q", -1, L.SD_ERR_INVALID_ARG), ("dtype", L.SD_F32, L.SD_ERR_UNSUPPORTED),
+    ("dtype", 7, L.SD_ERR_INVALID_ARG), ("scale", float("nan"), L.SD_ERR_INVALID_ARG),
+    ("scale", -1.0, L.SD_ERR_INVALID_ARG), ("scale", float("inf"), L.SD_ERR_INVALID_ARG),
+])
+def test_chunk_shape_errors(field, value, code):
+    assert chunk_ws(chunk_shape(**{field: value}))[0] == code
+    assert chunk(chunk_shape(**{field: value}), ws_bytes=1 << 40) == code
+
+
+def test_chunk_errors():
+    assert chunk_ws(None)[0] == L.SD_ERR_INVALID_ARG
+    assert L.lib().sd_chunk_attn_workspace_size(ctypes.byref(chunk_shape()), None) == L.SD_ERR_INVALID_ARG
+    assert chunk_ws(chunk_shape(num_q_heads=257, num_kv_heads=1))[0] == L.SD_ERR_UNSUPPORTED
+    assert chunk_ws(chunk_shape(num_q_heads=256, num_kv_heads=1))[0] == L.SD_OK
+    for sh in (chunk_shape(), chunk_shape(max_block=16, total_q=64)):  # the chunk kernel, the block kernels
+        rc, n = chunk_ws(sh)
+        assert rc == L.SD_OK and n > 0
+        for x in ("table", "q", "k", "v", "ctx", "len", "off", "out"):
+            assert chunk(sh, **{x: None}) == L.SD_ERR_INVALID_ARG, x
+        for x in ("q", "k", "v", "out"):
+            assert chunk(sh, **{x: 4104}) == L.SD_ERR_INVALID_ARG, x
+        assert chunk(sh, mask=2) == L.SD_ERR_INVALID_ARG
+        assert chunk(sh, ws=128) == L.SD_ERR_INVALID_ARG
+        assert chunk(sh, ws=None) == L.SD_ERR_INVALID_ARG
+        assert chunk(sh, ws_bytes=n - 1) == L.SD_ERR_WORKSPACE
+        for kw in (dict(page=8), dict(page=24), dict(pages=0), dict(most=255)):
+            assert chunk(sh, **kw) == L.SD_ERR_INVALID_ARG, kw
+    assert chunk(chunk_shape(num_seqs=0, total_q=0)) == L.SD_OK
+    assert chunk(chunk_shape(total_q=0), q=None) == L.SD_OK
+
+
+def _t(*shape, dt=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dt)
+
+
+def test_binding_refuses_wrong_shapes_and_host_tensors():
+    q, k, pos, f = _t(5, 4, 128), _t(5, 2, 128), _t(5, dt=torch.int32), _t(64, dt=torch.float32)
+    for bad in (dict(q=_t(6, 4, 128)), dict(q=_t(5, 4, 64)), dict(positions=pos[:4]), dict(q=_t(5, 512)), dict(q=None, k=None)):
+        with pytest.raises((ValueError, TypeError)):
+            L.qk_norm_rope(**{"q": q, "k": k, "positions": pos, "inv_freq": f, **bad})
+    with pytest.raises(ValueError, match="device tensor"):
+        L.qk_norm_rope(q, k, pos, f)
+    pool, table, lens, off = _t(9, 2, 16, 128), _t(3, 4, dt=torch.int32), _t(3, dt=torch.int32), _t(4, dt=torch.int32)
+    a = dict(q=q, k_new=k, v_new=k, k_pages=pool, v_pages=pool, block_table=table, ctx_lens=lens, q_offsets=off, inv_freq=f)
+    for bad in (dict(), dict(v_pages=pool[:4]), dict(k_pages=pool[0]), dict(q_offsets=lens)):
+        with pytest.raises((ValueError, TypeError)):
+            L.kv_append_rope_paged(**{**a, **bad})
+    c = dict(q=q, k_pages=pool, v_pages=pool, block_table=table, ctx_lens=lens, chunk_lens=lens, q_offsets=off,
+             mask_mode=0, max_ctx=0, max_chunk=5)
+    for bad in (dict(), dict(chunk_lens=off), dict(q=_t(5, 4, 64)), dict(out=_t(4, 4, 128))):
+        with pytest.raises((ValueError, TypeError)):
+            L.chunk_attn_paged(**{**c, **bad})
+
+
+def test_row_strides():
+    """_rows takes slices of packed rows and refuses heads apart, rows that overlap, other types."""
+    class OnDevice(torch.Tensor):
+        is_cuda = True
+    x = torch.zeros(6, 10 * 128, dtype=torch.bfloat16).as_subclass(OnDevice)
+    rows = lambda t, H, dt=torch.bfloat16: L._rows(t, "q", dt, t.device, None, H, 128)  # noqa: E731
+    assert rows(x[:, :512].unflatten(1, (4, 128)), 4) == 1280
+    assert rows(x[:1, :512].unflatten(1, (4, 128)), 4) == 512
+    assert rows(x[:, :128].unflatten(1, (1, 128)), 1) == 1280
+    with pytest.raises(ValueError, match="side by side"):
+        rows(x.unflatten(1, (10, 128))[:, ::2], 5)
+    with pytest.raises(ValueError, match="side by side"):
+        rows(x[:1, :512].expand(6, 512).unflatten(1, (4, 128)), 4)
+    with pytest.raises(TypeError):
+        rows(x[:, :512].unflatten(1, (4, 128)), 4, torch.float32)
