@@ -2,8 +2,8 @@
 // number of them, attend to their committed context and to the chunk itself.
 //
 // A query tile is P = 256 / G positions of one (sequence, kv head) with the G query heads of each, up
-// to 256 rows, so a key row that a workgroup fetches serves all of them.  A workgroup of four
-// wavefronts takes a tile, 64 rows a wavefront, and walks its keys 64 at a time:
+// to 256 rows, so a key row that a workgroup fetches serves all of them.  A workgroup of eight
+// wavefronts takes a tile, 32 rows a wavefront, and walks its keys 64 at a time:
 //   S^T = K Q^T    (32x32x16 bf16 matrix products, fp32 sums)
 //   P = exp2(S^T c - m), running row maximum m and row sum l in fp32
 //   O^T = O^T 2^(m_old - m) + V^T P^T   (P rounded to bf16 for the product; O^T fp32 in registers)
@@ -41,7 +41,7 @@ struct ChunkTile {
   static constexpr int ROWB = D * 2;                   // bytes of a key row
   static constexpr int CPR = ROWB / 16;                // 16-byte vectors of a row
   static constexpr int TILEB = kChunkKT * ROWB;        // bytes of a K (or V) tile
-  static constexpr int NV = 16 * CPR / 64;             // vectors a lane fetches of K (and of V): 16 rows a wavefront
+  static constexpr int NV = 16 * CPR / 64;             // vectors a lane fetches: 16 rows of K or of V a wavefront
   // A row's vectors are stored at their index XOR these, so that the 16 lanes an operand read serves at a
   // time touch distinct banks: 16 rows at one vector index of K, 4 rows at 4 indices of V.
   __device__ static int swz_k(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
@@ -79,8 +79,13 @@ __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int b, ChunkItem 
   return false;
 }
 
+// The running maximum may lag behind a row's scores by this much (log2 units) before the sums are
+// rescaled: weights then are at most 2^8 instead of 1, which changes no relative rounding, and the
+// rescaling of O, half as much work as the rest of the softmax, is left out of nearly every step.
+constexpr float kChunkLag = 8.f;
+
 template <int D>
-__global__ __launch_bounds__(256, 1) void chunk_attn_kernel(ChunkArgs a) {
+__global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
   using T = ChunkTile<D>;
   constexpr int NST = D / 16, NDT = D / 32, EB = 2;
   __shared__ __attribute__((aligned(1024))) char lds_raw[2][2 * T::TILEB];
@@ -92,56 +97,49 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_kernel(ChunkArgs a) {
   const int k1 = it.ctx + (a.causal ? it.p0 + np : it.B);  // keys [0, k1) are visible to some row
 
   // ---- query operands: element e of step st is dim st*16 + h*8 + e of row m ----
-  bf16x8 qop[2][NST];
-  int lim[2];  // keys the row sees
+  bf16x8 qop[NST];
+  const int m = wave * 32 + l32, mc = min(m, M - 1), mp = mc / a.G;  // rows past the tile: its last
+  const int lim = a.causal ? it.ctx + it.p0 + mp + 1 : k1;           // keys the row sees
+  {
+    const char *qrow = (const char *)a.q + ((size_t)(it.qoff + it.p0 + mp) * a.Hq + it.g * a.G + (mc - mp * a.G)) * D * EB;
 #pragma unroll
-  for (int nb = 0; nb < 2; ++nb) {
-    const int m = wave * 64 + nb * 32 + l32, mc = min(m, M - 1), p = mc / a.G;  // rows past the tile: its last
-    lim[nb] = a.causal ? it.ctx + it.p0 + p + 1 : k1;
-    const char *qrow = (const char *)a.q + ((size_t)(it.qoff + it.p0 + p) * a.Hq + it.g * a.G + (mc - p * a.G)) * D * EB;
-#pragma unroll
-    for (int st = 0; st < NST; ++st) qop[nb][st] = *(const bf16x8 *)(qrow + (st * 16 + h * 8) * EB);
+    for (int st = 0; st < NST; ++st) qop[st] = *(const bf16x8 *)(qrow + (st * 16 + h * 8) * EB);
   }
   // keys that all / some of the wavefront's rows see
-  const int pw0 = min(wave * 64, M - 1) / a.G, pw1 = min(wave * 64 + 63, M - 1) / a.G;
+  const int pw0 = min(wave * 32, M - 1) / a.G, pw1 = min(wave * 32 + 31, M - 1) / a.G;
   const int vis_all = a.causal ? it.ctx + it.p0 + pw0 + 1 : k1;
-  const int vis_any = wave * 64 >= M ? 0 : a.causal ? it.ctx + it.p0 + pw1 + 1 : k1;
+  const int vis_any = wave * 32 >= M ? 0 : a.causal ? it.ctx + it.p0 + pw1 + 1 : k1;
 
-  f32x16 oacc[2][NDT];
-  float m_run[2], l_run[2];
+  f32x16 oacc[NDT];
+  float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-  for (int nb = 0; nb < 2; ++nb) {
-    m_run[nb] = -INFINITY;
-    l_run[nb] = 0.f;
+  for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) oacc[nb][dt][i] = 0.f;
-  }
+    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
 
-  // ---- key and value tiles: wavefront w fetches rows 16w .. 16w + 15 of both, which lie in one page ----
+  // ---- key and value tiles: wavefronts 0-3 fetch rows 16w .. 16w + 15 of K, 4-7 those of V; they lie in one page ----
   const int *table = a.block_table + (size_t)it.s * a.max_pages;
-  v4u32 kreg[T::NV], vreg[T::NV];  // a vector type: an array of the u32x4 struct is copied through private memory
+  const bool isv = wave >= 4;
+  const int frow = (wave & 3) * 16;
+  const char *pool = (const char *)(isv ? a.v : a.k);
+  v4u32 reg[T::NV];  // a vector type: an array of the u32x4 struct is copied through private memory
   const int pmask = (1 << a.page_log2) - 1;
   auto fetch = [&](int key0) {  // rows past the last key re-read it (rows behind it may hold anything)
-    const int kw = __builtin_amdgcn_readfirstlane(min(key0 + wave * 16, k1 - 1));
+    const int kw = __builtin_amdgcn_readfirstlane(min(key0 + frow, k1 - 1));
     const int pg = min(max(ld_uniform(table, min(kw >> a.page_log2, a.max_pages - 1)), 0), a.num_pages - 1);
-    const size_t page = ((((size_t)pg * a.Hkv + it.g) << a.page_log2)) * T::ROWB;
+    const char *page = pool + ((((size_t)pg * a.Hkv + it.g) << a.page_log2)) * T::ROWB;
 #pragma unroll
     for (int i = 0; i < T::NV; ++i) {
       const int v = i * 64 + lane, r = v / T::CPR, c = v % T::CPR;
-      const int key = min(key0 + wave * 16 + r, k1 - 1);
-      const size_t at = page + (unsigned)((key & pmask) * T::ROWB + c * 16);
-      kreg[i] = *(const v4u32 *)((const char *)a.k + at);
-      vreg[i] = *(const v4u32 *)((const char *)a.v + at);
+      const int key = min(key0 + frow + r, k1 - 1);
+      reg[i] = *(const v4u32 *)(page + (unsigned)((key & pmask) * T::ROWB + c * 16));
     }
   };
   auto stash = [&](char *stage) {
 #pragma unroll
     for (int i = 0; i < T::NV; ++i) {
-      const int v = i * 64 + lane, r = wave * 16 + v / T::CPR, c = v % T::CPR;
-      *(v4u32 *)(stage + r * T::ROWB + ((c ^ T::swz_k(r)) << 4)) = kreg[i];
-      *(v4u32 *)(stage + T::TILEB + r * T::ROWB + ((c ^ T::swz_v(r)) << 4)) = vreg[i];
+      const int v = i * 64 + lane, r = frow + v / T::CPR, c = v % T::CPR;
+      *(v4u32 *)(stage + (isv ? T::TILEB : 0) + r * T::ROWB + ((c ^ (isv ? T::swz_v(r) : T::swz_k(r))) << 4)) = reg[i];
     }
   };
   // V^T operand: lane l of a 16-lane group reads 4 dims of key row (l % 16) / 4 of four and receives, of
@@ -159,103 +157,86 @@ __global__ __launch_bounds__(256, 1) void chunk_attn_kernel(ChunkArgs a) {
     if (t + 1 < ntiles) fetch(kt + kChunkKT);
     if (kt >= vis_any) continue;  // uniform per wavefront
 
-    f32x16 sacc[2][2];  // [nb][kb]: register i is key kb*32 + 8*(i/4) + 4h + i%4 of row nb*32 + l32
+    f32x16 sacc[2];  // [kb]: register i is key kb*32 + 8*(i/4) + 4h + i%4 of row l32
 #pragma unroll
-    for (int nb = 0; nb < 2; ++nb)
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sacc[nb][kb][i] = 0.f;
+      for (int i = 0; i < 16; ++i) sacc[kb][i] = 0.f;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int st = 0; st < NST; ++st) {
         const int r = kb * 32 + l32;
         const bf16x8 kf = *(const bf16x8 *)(stage + r * T::ROWB + (((2 * st + h) ^ T::swz_k(r)) << 4));
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-          sacc[nb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qop[nb][st], sacc[nb][kb], 0, 0, 0);
+        sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qop[st], sacc[kb], 0, 0, 0);
       }
     if (kt + kChunkKT > vis_all) {
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (kt + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= lim[nb]) sacc[nb][kb][i] = -INFINITY;
-    }
-    bf16x8 pop[2][4];
-#pragma unroll
-    for (int nb = 0; nb < 2; ++nb) {
-      float tmax = -INFINITY;
-#pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sacc[nb][kb][i]);
-      const float2 pm = pair_x32(tmax);
-      const float mnew = fmaxf(m_run[nb], fmaxf(pm.x, pm.y) * a.scale_log2);
-      const float muse = mnew == -INFINITY ? 0.f : mnew;
-      float psum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sacc[nb][kb][i] = fast_exp2(fmaf(sacc[nb][kb][i], a.scale_log2, -muse));
-          psum += sacc[nb][kb][i];
-        }
-      if (__any(mnew != m_run[nb])) {
-        const float alpha = fast_exp2(m_run[nb] - muse);
-        l_run[nb] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) oacc[nb][dt] *= alpha;
-      }
-      m_run[nb] = mnew;
-      l_run[nb] += psum;
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const f32x16 &p = sacc[nb][ks >> 1];
-        const int i0 = 8 * (ks & 1);
-        const u32x4 raw{cvt_pk_bf16(p[i0], p[i0 + 1]), cvt_pk_bf16(p[i0 + 2], p[i0 + 3]),
-                        cvt_pk_bf16(p[i0 + 4], p[i0 + 5]), cvt_pk_bf16(p[i0 + 6], p[i0 + 7])};
-        pop[nb][ks] = __builtin_bit_cast(bf16x8, raw);
-      }
+        for (int i = 0; i < 16; ++i)
+          if (kt + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= lim) sacc[kb][i] = -INFINITY;
     }
+    float tmax = -INFINITY;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sacc[kb][i]);
+    const float2 pm = pair_x32(tmax);
+    const float mt = fmaxf(pm.x, pm.y) * a.scale_log2;
+    if (__any(mt > m_run + kChunkLag)) {
+      const float mnew = fmaxf(m_run, mt);
+      const float alpha = mnew == -INFINITY ? 1.f : fast_exp2(m_run - mnew);
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= alpha;
+      m_run = mnew;
+    }
+    const float muse = m_run == -INFINITY ? 0.f : m_run;
+    float psum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sacc[kb][i] = fast_exp2(fmaf(sacc[kb][i], a.scale_log2, -muse));
+        psum[kb] += sacc[kb][i];
+      }
+    l_run += psum[0] + psum[1];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const f32x16 &p = sacc[ks >> 1];
+      const int i0 = 8 * (ks & 1);
+      const u32x4 raw{cvt_pk_bf16(p[i0], p[i0 + 1]), cvt_pk_bf16(p[i0 + 2], p[i0 + 3]),
+                      cvt_pk_bf16(p[i0 + 4], p[i0 + 5]), cvt_pk_bf16(p[i0 + 6], p[i0 + 7])};
+      const bf16x8 pop = __builtin_bit_cast(bf16x8, raw);
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt) {
         s16x4c vv[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int r = ks * 16 + u * 8 + vrow;
-          const char *p = stage + T::TILEB + r * T::ROWB + (((4 * dt + vcol) ^ T::swz_v(r)) << 4) + ((lane & 1) << 3);
-          vv[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4c SDB_LDS *)p);
+          const char *p8 = stage + T::TILEB + r * T::ROWB + (((4 * dt + vcol) ^ T::swz_v(r)) << 4) + ((lane & 1) << 3);
+          vv[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4c SDB_LDS *)p8);
         }
         const s16x8c v8 = {vv[0][0], vv[0][1], vv[0][2], vv[0][3], vv[1][0], vv[1][1], vv[1][2], vv[1][3]};
-#pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-          oacc[nb][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pop[nb][ks], oacc[nb][dt], 0, 0, 0);
+        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pop, oacc[dt], 0, 0, 0);
       }
+    }
   }
 
-  // ---- output: register i of oacc[nb][dt] is dim dt*32 + 8*(i/4) + 4h + i%4 of row nb*32 + l32 ----
+  // ---- output: register i of oacc[dt] is dim dt*32 + 8*(i/4) + 4h + i%4 of row l32 ----
+  const float2 pl = pair_x32(l_run);
+  const float inv = 1.f / (pl.x + pl.y);
+  if (m >= M) return;
+  char *orow = (char *)a.out + ((size_t)(it.qoff + it.p0 + mp) * a.Hq + it.g * a.G + (m - mp * a.G)) * D * EB;
 #pragma unroll
-  for (int nb = 0; nb < 2; ++nb) {
-    const float2 pl = pair_x32(l_run[nb]);
-    const float inv = 1.f / (pl.x + pl.y);
-    const int m = wave * 64 + nb * 32 + l32, p = m / a.G;
-    if (m >= M) continue;
-    char *orow = (char *)a.out + ((size_t)(it.qoff + it.p0 + p) * a.Hq + it.g * a.G + (m - p * a.G)) * D * EB;
+  for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const f32x16 &o = oacc[nb][dt];
-        *(uint2 *)(orow + (dt * 32 + c * 8 + h * 4) * EB) =
-            uint2{cvt_pk_bf16(o[4 * c] * inv, o[4 * c + 1] * inv), cvt_pk_bf16(o[4 * c + 2] * inv, o[4 * c + 3] * inv)};
-      }
-  }
+    for (int c = 0; c < 4; ++c) {
+      const f32x16 &o = oacc[dt];
+      *(uint2 *)(orow + (dt * 32 + c * 8 + h * 4) * EB) =
+          uint2{cvt_pk_bf16(o[4 * c] * inv, o[4 * c + 1] * inv), cvt_pk_bf16(o[4 * c + 2] * inv, o[4 * c + 3] * inv)};
+    }
 }
 
 }  // namespace sdb

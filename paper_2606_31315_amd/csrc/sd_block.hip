@@ -774,8 +774,8 @@ int sd_chunk_attn_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_
   const float scale = sh->scale > 0.f ? sh->scale : 1.0f / sqrtf((float)sh->head_dim);
   a.scale_log2 = scale * 1.4426950408889634f;
   const unsigned grid = (unsigned)((sh->total_q / a.P + sh->num_seqs) * sh->num_kv_heads);
-  if (sh->head_dim == 128) hipLaunchKernelGGL(sdb::chunk_attn_kernel<128>, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(sdb::chunk_attn_kernel<64>, dim3(grid), dim3(256), 0, (hipStream_t)stream, a);
+  if (sh->head_dim == 128) hipLaunchKernelGGL(sdb::chunk_attn_kernel<128>, dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(sdb::chunk_attn_kernel<64>, dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
   return check_launch("sd_chunk_attn_paged");
 }
 
