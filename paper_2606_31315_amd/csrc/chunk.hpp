@@ -17,12 +17,133 @@
 
 namespace sdb {
 
+constexpr int kChunkRows = 256;  // query rows of a tile
+constexpr int kChunkKT = 64;     // keys of a step
+
+// ---- plan --------------------------------------------------------------------------
+// Query tiles have from one key step to thousands, and their number seldom fits the device.  A small
+// launch orders the sequences by their longest tile, longest first, deals their kv heads to eight
+// queues, one per XCD, and decides which tiles are cut into pieces of keys: those near the end of the
+// order, whose length the work behind them could not even out.  Workgroups take the next item of
+// their XCD's queue, and of another when that is empty.  The tiles of one kv head are neighbours in a queue, so
+// the workgroups of an XCD walk the same keys at about the same time and fetch them once into its L2 (a chunk of
+// 2048 rows at 65536 keys, 8 query heads to a kv head: 2.21 ms with an equal share of a line of all tiles for
+// every workgroup, whose walks are spread over the keys, 1.94 ms in step).  Pieces file their
+// unnormalised sums, and a third launch joins them.
+constexpr int kChunkQueues = 8;
+constexpr int kChunkGrid = 256;       // workgroups at most: one fills a CU
+constexpr int kChunkSlots = 1024;     // pieces at most
+constexpr int kChunkSortSeqs = 4096;  // batches past this keep their order
+constexpr int kChunkPieceCost = 128;  // keys' worth of starting and ending an item
+constexpr int kChunkMinPiece = 256;   // keys of a piece at least
+constexpr int kChunkFew = 128;        // batches of less than this many tiles are cut throughout
+constexpr int kChunkSpread = 64;      // else a tile is cut where less than this many of its kind are left
+constexpr int kChunkEndPieces = 3;    // into this many pieces
+constexpr int kChunkPieceExtra = 512; // keys' worth of cutting: sums filed and joined
+
+// Relative time of a key by the tile's rows: wavefronts without rows leave theirs to the others.
+SDB_HD int chunk_weight(int rows) { return plan_max((rows + 31) / 32, 3); }
+
+struct ChunkSeq {
+  int ctx, B, P, G, causal;
+  SDB_HD int tiles() const { return B > 0 ? (B + P - 1) / P : 0; }
+  SDB_HD int rows(int j) const { return plan_min(P, B - P * j) * G; }           // of tile j
+  SDB_HD int keys(int j) const { return ctx + (causal ? plan_min(P * (j + 1), B) : B); }
+  // Work of tile j, and of the tiles before it (which are all full): whole numbers, below 2^53 (the host checks).
+  SDB_HD double units(int j) const { return (double)chunk_weight(rows(j)) * ((double)keys(j) + kChunkPieceCost); }
+  SDB_HD double before(int j) const {
+    const double n = j, each = (double)(causal ? ctx : ctx + B) + kChunkPieceCost;
+    return chunk_weight(P * G) * (n * each + (causal ? n * (n + 1) / 2 * P : 0));
+  }
+  SDB_HD double all_units() const { const int n = tiles(); return n ? before(n - 1) + units(n - 1) : 0; }
+  SDB_HD bool few() const { return B > 0 && B * G <= 64; }  // rows: bound by its keys' way from memory
+  SDB_HD double longest() const {  // the last tile may have few rows
+    const int n = tiles();
+    const double u = n ? units(n - 1) : 0, v = n > 1 ? units(n - 2) : 0;
+    return u > v ? u : v;
+  }
+};
+
+// Tiles 0 .. js - 1 of each of a sequence's heads are cut into np pieces, the others are whole.  after: work of the
+// sequences behind it, total: of the batch.
+struct ChunkSplit {
+  int js, np;
+};
+SDB_HD ChunkSplit chunk_split(const ChunkSeq &q, int Hkv, double after, double total) {
+  const int nt = q.tiles();
+  int lo = 0, hi = nt;
+  while (lo < hi) {  // the first js that is not cut (a search, as if there were one)
+    const int j = lo + (hi - lo) / 2;
+    if (total < kChunkFew * q.units(j) || after + Hkv * (q.before(j) + q.units(j)) < kChunkSpread * q.units(j)) lo = j + 1;
+    else hi = j;
+  }
+  if (lo == 0) return ChunkSplit{0, 1};
+  double longest = q.units(lo - 1);
+  if (lo > 1 && q.units(lo - 2) > longest) longest = q.units(lo - 2);
+  const double tiles = total / longest;  // tiles like this one
+  int np = 1;
+  if (tiles >= kChunkFew) {  // the end of a long batch
+    np = kChunkEndPieces;
+  } else {  // all of it: the number of rounds over the device, of as many pieces as fit it, that ends first
+    const double extra = (double)chunk_weight(kChunkRows) * kChunkPieceExtra;
+    double best = longest;
+    for (int k = 1; k <= 4; ++k) {
+      const int n = plan_min((int)(kChunkGrid * k / tiles), 64);
+      const double t = k * (longest / plan_max(n, 1) + extra);
+      if (n > 1 && t < best) {
+        best = t;
+        np = n;
+      }
+    }
+  }
+  const int most = (int)(longest / ((double)chunk_weight(kChunkRows) * kChunkMinPiece));
+  if (np > most) np = most;
+  return np > 1 ? ChunkSplit{lo, np} : ChunkSplit{0, 1};
+}
+// First key of piece i of np of n keys (i = np: n): whole steps, evenly; a piece may be empty.
+SDB_HD int chunk_piece(int n, int np, int i) {
+  const long long steps = (n + kChunkKT - 1) / kChunkKT;
+  return i == np ? n : (int)(steps * i / np) * kChunkKT;
+}
+
+// What the plan says of a sequence, in the order of the queues.
+struct ChunkEntry {
+  int s, ctx, B, qoff;
+  int nt, js, np, slot0;  // slot0: partial slot of piece 0 of tile 0 of head 0
+  int items;              // of each of its heads
+  int merge0;             // first of its cut tiles in the list of the merge
+  int pad[2];
+  // Item i of a head: the whole tiles from the last on, then the first pieces of the others, the second ones, ...
+  SDB_HD int whole() const { return nt - js; }
+  SDB_HD int tile(int i) const { return i < whole() ? nt - 1 - i : js - 1 - (i - whole()) % js; }
+  SDB_HD int piece(int i) const { return i < whole() ? -1 : (i - whole()) / js; }  // -1: a whole tile
+  SDB_HD int slot(int g, int j, int p) const { return slot0 + (g * js + j) * np + p; }
+};
+// Kv head g of the r-th sequence is group r * Hkv + g; queue x holds groups x, x + 8, ...
+SDB_HD int chunk_groups(long long groups, int x) { return groups > x ? (int)((groups - x + kChunkQueues - 1) / kChunkQueues) : 0; }
+
+// A cut tile, for the merge.
+struct ChunkMerge {
+  int row0, g, rows, keys, np, slot, pad[2];  // row0: its first position in q and out
+};
+
+struct ChunkHead {
+  struct {
+    int v, pad[63];
+  } next[kChunkQueues];     // items taken: a line each, atomics on one line wait for each other
+  int count[kChunkQueues];  // items
+  int merges;
+};
+
+#if defined(__HIPCC__)
+
+}  // namespace sdb
+#include <type_traits>
+namespace sdb {
+
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4c __attribute__((ext_vector_type(4)));
 typedef short s16x8c __attribute__((ext_vector_type(8)));
-
-constexpr int kChunkRows = 256;  // query rows of a tile
-constexpr int kChunkKT = 64;     // keys of a step
 
 struct ChunkArgs {
   const void *q;             // [total_q, Hq, D]
@@ -34,6 +155,15 @@ struct ChunkArgs {
   int page_log2, max_pages, num_pages;
   int causal;
   float scale_log2;          // softmax scale * log2(e)
+  int slots, grid;           // partial slots, workgroups
+  // workspace
+  ChunkHead *head;
+  ChunkEntry *entries;       // [S]
+  int *order;                // [S] the plan's own
+  int *prefix;               // [8, ceil(S Hkv / 8)] first item of each group of a queue
+  ChunkMerge *merges;        // [slots / 2]
+  float *part_o;             // [slots, 256, D] unnormalised sums
+  float2 *part_ml;           // [slots, 256] (reference of the weights in log2 units, row sum)
 };
 
 template <int D>
@@ -41,6 +171,7 @@ struct ChunkTile {
   static constexpr int ROWB = D * 2;                   // bytes of a key row
   static constexpr int CPR = ROWB / 16;                // 16-byte vectors of a row
   static constexpr int TILEB = kChunkKT * ROWB;        // bytes of a K (or V) tile
+  static constexpr int STAGEB = 2 * TILEB;             // K, then V
   static constexpr int NV = 16 * CPR / 64;             // vectors a lane fetches: 16 rows of K or of V a wavefront
   // A row's vectors are stored at their index XOR these, so that the 16 lanes an operand read serves at a
   // time touch distinct banks: 16 rows at one vector index of K, 4 rows at 4 indices of V.
@@ -48,35 +179,171 @@ struct ChunkTile {
   __device__ static int swz_v(int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
 };
 
-struct ChunkItem {
-  int s, g, ctx, B, qoff, p0;  // p0: the tile's first position in the chunk
-};
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs &a, int s) {
+  return ChunkSeq{a.ctx_lens[s], a.chunk_lens[s], a.P, a.G, a.causal};
+}
 
-// Tile b of the batch: sequences in order, within one the kv heads in order, within one the tiles from
-// the last to the first (under the causal mask the last has the most keys).
-__device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int b, ChunkItem &it) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int c0 = 0; c0 < a.S; c0 += 64) {
-    const int k = min(c0 + lane, a.S - 1);  // clamped: no per-load branch
-    const int ctx = a.ctx_lens[k], B = a.chunk_lens[k], off = a.q_offsets[k];
-    const int nt = c0 + lane < a.S && B > 0 ? (B + a.P - 1) / a.P : 0;
-    const int items = nt * a.Hkv, incl = before + wave_scan_i(items);
-    const unsigned long long hit = __ballot(incl > b && incl - items <= b);
-    if (hit) {
-      const int l = __ffsll((long long)hit) - 1;  // wave-uniform
-      it.s = c0 + l;
-      it.ctx = __builtin_amdgcn_readlane(ctx, l);
-      it.B = __builtin_amdgcn_readlane(B, l);
-      it.qoff = __builtin_amdgcn_readlane(off, l);
-      const int n = __builtin_amdgcn_readlane(nt, l), r = b - __builtin_amdgcn_readlane(incl - items, l);
-      it.g = r / n;
-      it.p0 = (n - 1 - (r - it.g * n)) * a.P;
-      return true;
+// The plan, by one workgroup.  Sums of work are whole numbers in doubles and every order is fixed: the same lengths
+// give the same plan.
+constexpr int kChunkPlanThreads = 1024;
+__global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
+  __shared__ float key[kChunkSortSeqs], place[kChunkSortSeqs];
+  __shared__ double sums[kChunkPlanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.S;
+  const bool sorted = S <= kChunkSortSeqs;
+  // the batch's work; sequences by their longest tile, those of few rows marked by the sign
+  double mine = 0;
+  for (int s = tid; s < S; s += kChunkPlanThreads) {
+    const ChunkSeq q = chunk_seq(a, s);
+    mine += q.all_units() * a.Hkv;
+    if (sorted) {
+      key[s] = (float)q.longest() * (q.few() ? -1.f : 1.f);
+      place[s] = (float)q.all_units();
+    } else {
+      a.order[s] = s;
     }
-    before = __builtin_amdgcn_readlane(incl, 63);
   }
-  return false;
+  mine = wave_sum_d(mine);
+  if (lane == 0) sums[wave] = mine;
+  __syncthreads();
+  double total = 0;
+  for (int w = 0; w < kChunkPlanThreads / 64; ++w) total += sums[w];
+  if (sorted) {
+    // Each kind longest first, and the two interleaved by the share of their work that is done by then.
+    float at[kChunkSortSeqs / kChunkPlanThreads];
+#pragma unroll
+    for (int i = 0; i < kChunkSortSeqs / kChunkPlanThreads; ++i) {
+      const int s = tid + i * kChunkPlanThreads;
+      if (s >= S) break;
+      const float k = key[s];
+      float before = 0.f, all = 0.f;
+      for (int t = 0; t < S; ++t) {
+        const float u = key[t], w = place[t];
+        const bool same = (u < 0.f) == (k < 0.f);
+        all += same ? w : 0.f;
+        before += same && (fabsf(u) > fabsf(k) || (u == k && t < s)) ? w : 0.f;
+      }
+      at[i] = all > 0.f ? (before + 0.5f * place[s]) / all : 2.f;  // sequences without rows come last
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kChunkSortSeqs / kChunkPlanThreads; ++i)
+      if (tid + i * kChunkPlanThreads < S) place[tid + i * kChunkPlanThreads] = at[i];
+    __syncthreads();
+    for (int s = tid; s < S; s += kChunkPlanThreads) {
+      const float k = place[s];
+      int rank = 0;
+      for (int t = 0; t < S; ++t) rank += place[t] < k || (place[t] == k && t < s);
+      a.order[rank] = s;
+    }
+  }
+  __threadfence_block();
+  __syncthreads();
+  // entries from the last to the first, 64 a round: what lies behind each is known then
+  if (wave == 0) {
+    double after = 0, slots = 0;
+    int merges = 0;
+    for (int c0 = (S - 1) / 64 * 64; c0 >= 0; c0 -= 64) {
+      const int r = min(c0 + lane, S - 1);
+      const bool live = c0 + lane < S;
+      ChunkEntry e{};
+      e.s = a.order[r];
+      const ChunkSeq q = chunk_seq(a, e.s);
+      e.ctx = q.ctx;
+      e.B = q.B;
+      e.qoff = a.q_offsets[e.s];
+      e.nt = live ? q.tiles() : 0;
+      double excl;
+      const double units = live ? q.all_units() * a.Hkv : 0.0, incl = wave_scan_d(units, &excl), all = readlane_d(incl, 63);
+      ChunkSplit sp = e.nt ? chunk_split(q, a.Hkv, after + (all - incl), total) : ChunkSplit{0, 1};
+      const double want = sp.np > 1 ? (double)sp.js * sp.np * a.Hkv : 0.0, wi = wave_scan_d(want, &excl), wall = readlane_d(wi, 63);
+      const double slot0 = slots + (wall - wi);  // of the sequences behind
+      if (slot0 + want > a.slots) sp = ChunkSplit{0, 1};
+      e.js = sp.js;
+      e.np = sp.np;
+      e.slot0 = sp.js ? (int)slot0 : 0;
+      e.items = e.nt - sp.js + sp.js * sp.np;
+      const int mi = wave_scan_i(sp.js * a.Hkv), mall = __builtin_amdgcn_readlane(mi, 63);
+      e.merge0 = merges + mall - mi;
+      if (live) a.entries[r] = e;
+      after += all;
+      slots += wall;
+      merges += mall;
+    }
+    if (lane == 0) a.head->merges = merges;
+  }
+  __threadfence_block();
+  __syncthreads();
+  if (wave < kChunkQueues) {  // a queue each
+    const int x = wave, n = chunk_groups((long long)S * a.Hkv, x), stride = (S * a.Hkv + kChunkQueues - 1) / kChunkQueues;
+    int base = 0;
+    for (int k0 = 0; k0 < n; k0 += 64) {
+      const int k = min(k0 + lane, n - 1);
+      const int items = k0 + lane < n ? a.entries[(x + kChunkQueues * k) / a.Hkv].items : 0;
+      const int incl = wave_scan_i(items);
+      if (k0 + lane < n) a.prefix[x * stride + k] = base + incl - items;
+      base += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (lane == 0) {
+      a.head->next[x].v = ((int)a.grid - x + kChunkQueues - 1) / kChunkQueues;  // each workgroup's first item is its own
+      a.head->count[x] = base;
+    }
+  } else {  // the list of cut tiles, the sequences that have some in turn
+    const int t0 = tid - kChunkQueues * 64, nt0 = kChunkPlanThreads - kChunkQueues * 64;
+    for (int c0 = 0; c0 < S; c0 += 64) {
+      const ChunkEntry e = a.entries[min(c0 + lane, S - 1)];
+      unsigned long long cut = __ballot(c0 + lane < S && e.js > 0);
+      while (cut) {
+        const int l = __ffsll((long long)cut) - 1;
+        cut &= cut - 1;
+        ChunkEntry u{};
+        u.ctx = __builtin_amdgcn_readlane(e.ctx, l);
+        u.B = __builtin_amdgcn_readlane(e.B, l);
+        u.qoff = __builtin_amdgcn_readlane(e.qoff, l);
+        u.js = __builtin_amdgcn_readlane(e.js, l);
+        u.np = __builtin_amdgcn_readlane(e.np, l);
+        u.slot0 = __builtin_amdgcn_readlane(e.slot0, l);
+        u.merge0 = __builtin_amdgcn_readlane(e.merge0, l);
+        const ChunkSeq q{u.ctx, u.B, a.P, a.G, a.causal};
+        for (int t = t0; t < u.js * a.Hkv; t += nt0) {
+          const int g = t / u.js, j = t - g * u.js;
+          a.merges[u.merge0 + t] = ChunkMerge{u.qoff + j * a.P, g, q.rows(j), q.keys(j), u.np, u.slot(g, j, 0), {0, 0}};
+        }
+      }
+    }
+  }
+}
+
+// Another queue that has items left, or -1.  (One that was empty once stays so.)
+__device__ __forceinline__ int chunk_other(const ChunkArgs &a, int x) {
+  int next[kChunkQueues], found = -1;
+#pragma unroll
+  for (int o = 1; o < kChunkQueues; ++o)
+    next[o] = __hip_atomic_load(&a.head->next[x ^ o].v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+  for (int o = 1; o < kChunkQueues; ++o)
+    if (next[o] < a.head->count[x ^ o]) found = x ^ o;
+  return found;
+}
+__device__ __forceinline__ int chunk_take(const ChunkArgs &a, int x) {
+  return __hip_atomic_fetch_add(&a.head->next[x].v, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The group of queue x that holds item i: the last whose first item is at most i.
+__device__ __forceinline__ int chunk_group(const ChunkArgs &a, int x, int i, int *first) {
+  const int lane = threadIdx.x & 63;
+  const int n = chunk_groups((long long)a.S * a.Hkv, x), stride = (a.S * a.Hkv + kChunkQueues - 1) / kChunkQueues;
+  int k = 0;
+  for (int k0 = 0; k0 < n; k0 += 64) {
+    const int p = a.prefix[x * stride + min(k0 + lane, n - 1)];
+    const unsigned long long le = __ballot(k0 + lane < n && p <= i);
+    if (!le) break;
+    const int l = 63 - __clzll((long long)le);
+    k = k0 + l;
+    *first = __builtin_amdgcn_readlane(p, l);
+    if (l < 63) break;
+  }
+  return x + kChunkQueues * k;
 }
 
 // The running maximum may lag behind a row's scores by this much (log2 units) before the sums are
@@ -84,159 +351,351 @@ __device__ __forceinline__ bool chunk_item(const ChunkArgs &a, int b, ChunkItem 
 // rescaling of O, half as much work as the rest of the softmax, is left out of nearly every step.
 constexpr float kChunkLag = 8.f;
 
+// Fetches 16 bytes a lane from base + off to LDS bytes dst + 16 * lane.  As assembly without outputs: the
+// compiler knows of no transfer in flight and so makes no LDS read wait for all of them, as it does
+// after the builtin; the waits are chunk_phase_end's.  (Its own waits for vector loads count the transfers
+// as well, so they only grow stricter.)
+__device__ __forceinline__ void chunk_load_lds(const char *base, unsigned off, unsigned dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base));
+}
+
+// Ends a phase: this wavefront's LDS reads are done, and all but its N youngest transfers (N < 0: no
+// matter which), before the barrier.  (__syncthreads would wait for every transfer in flight.)
+template <int N>
+__device__ __forceinline__ void chunk_phase_end() {
+  if constexpr (N < 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <int V>
+using Int = std::integral_constant<int, V>;
+
 template <int D>
 __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
   using T = ChunkTile<D>;
   constexpr int NST = D / 16, NDT = D / 32, EB = 2;
-  __shared__ __attribute__((aligned(1024))) char lds_raw[2][2 * T::TILEB];
-  ChunkItem it;
-  if (!chunk_item(a, blockIdx.x, it)) return;
+  __shared__ __attribute__((aligned(1024))) char stages[4 * T::STAGEB];  // a K and a V tile each
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int np = min(a.P, it.B - it.p0), M = np * a.G;  // the tile's positions and rows
-  const int k1 = it.ctx + (a.causal ? it.p0 + np : it.B);  // keys [0, k1) are visible to some row
-
-  // ---- query operands: element e of step st is dim st*16 + h*8 + e of row m ----
-  bf16x8 qop[NST];
-  const int m = wave * 32 + l32, mc = min(m, M - 1), mp = mc / a.G;  // rows past the tile: its last
-  const int lim = a.causal ? it.ctx + it.p0 + mp + 1 : k1;           // keys the row sees
-  {
-    const char *qrow = (const char *)a.q + ((size_t)(it.qoff + it.p0 + mp) * a.Hq + it.g * a.G + (mc - mp * a.G)) * D * EB;
-#pragma unroll
-    for (int st = 0; st < NST; ++st) qop[st] = *(const bf16x8 *)(qrow + (st * 16 + h * 8) * EB);
-  }
-  // keys that all / some of the wavefront's rows see
-  const int pw0 = min(wave * 32, M - 1) / a.G, pw1 = min(wave * 32 + 31, M - 1) / a.G;
-  const int vis_all = a.causal ? it.ctx + it.p0 + pw0 + 1 : k1;
-  const int vis_any = wave * 32 >= M ? 0 : a.causal ? it.ctx + it.p0 + pw1 + 1 : k1;
-
-  f32x16 oacc[NDT];
-  float m_run = -INFINITY, l_run = 0.f;
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-
-  // ---- key and value tiles: wavefronts 0-3 fetch rows 16w .. 16w + 15 of K, 4-7 those of V; they lie in one page ----
-  const int *table = a.block_table + (size_t)it.s * a.max_pages;
-  const bool isv = wave >= 4;
-  const int frow = (wave & 3) * 16;
-  const char *pool = (const char *)(isv ? a.v : a.k);
-  v4u32 reg[T::NV];  // a vector type: an array of the u32x4 struct is copied through private memory
-  const int pmask = (1 << a.page_log2) - 1;
-  auto fetch = [&](int key0) {  // rows past the last key re-read it (rows behind it may hold anything)
-    const int kw = __builtin_amdgcn_readfirstlane(min(key0 + frow, k1 - 1));
-    const int pg = min(max(ld_uniform(table, min(kw >> a.page_log2, a.max_pages - 1)), 0), a.num_pages - 1);
-    const char *page = pool + ((((size_t)pg * a.Hkv + it.g) << a.page_log2)) * T::ROWB;
-#pragma unroll
-    for (int i = 0; i < T::NV; ++i) {
-      const int v = i * 64 + lane, r = v / T::CPR, c = v % T::CPR;
-      const int key = min(key0 + frow + r, k1 - 1);
-      reg[i] = *(const v4u32 *)(page + (unsigned)((key & pmask) * T::ROWB + c * 16));
-    }
-  };
-  auto stash = [&](char *stage) {
-#pragma unroll
-    for (int i = 0; i < T::NV; ++i) {
-      const int v = i * 64 + lane, r = frow + v / T::CPR, c = v % T::CPR;
-      *(v4u32 *)(stage + (isv ? T::TILEB : 0) + r * T::ROWB + ((c ^ (isv ? T::swz_v(r) : T::swz_k(r))) << 4)) = reg[i];
-    }
-  };
-  // V^T operand: lane l of a 16-lane group reads 4 dims of key row (l % 16) / 4 of four and receives, of
-  // dim 16 * ((l / 16) % 2) + l % 16 of the 32, those four keys.
-  const int vrow = 4 * h + ((lane & 15) >> 2);
-  const int vcol = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);  // 16-byte vector of the 32 dims
-
-  const int ntiles = (k1 + kChunkKT - 1) / kChunkKT;
-  fetch(0);
-  for (int t = 0; t < ntiles; ++t) {
-    char *stage = lds_raw[t & 1];
-    stash(stage);
-    __syncthreads();  // the tile is there for every wavefront
-    const int kt = t * kChunkKT;
-    if (t + 1 < ntiles) fetch(kt + kChunkKT);
-    if (kt >= vis_any) continue;  // uniform per wavefront
-
-    f32x16 sacc[2];  // [kb]: register i is key kb*32 + 8*(i/4) + 4h + i%4 of row l32
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sacc[kb][i] = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int st = 0; st < NST; ++st) {
-        const int r = kb * 32 + l32;
-        const bf16x8 kf = *(const bf16x8 *)(stage + r * T::ROWB + (((2 * st + h) ^ T::swz_k(r)) << 4));
-        sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qop[st], sacc[kb], 0, 0, 0);
+  __shared__ int ticket[2];
+  // Workgroups take the items of their XCD's queue, then those of the others.  Any may take any item: no result
+  // depends on which.  The next item is asked for at the end of one.
+  int queue = blockIdx.x % kChunkQueues, ahead = blockIdx.x / kChunkQueues;
+  for (;;) {  // one pass per item
+    if (tid == 0) {
+      while (ahead >= a.head->count[queue]) {
+        queue = chunk_other(a, queue);
+        if (queue < 0) break;
+        ahead = chunk_take(a, queue);
       }
-    if (kt + kChunkKT > vis_all) {
+      ticket[0] = queue;
+      ticket[1] = ahead;
+    }
+    __syncthreads();
+    const int x = __builtin_amdgcn_readfirstlane(ticket[0]), item = __builtin_amdgcn_readfirstlane(ticket[1]);
+    __syncthreads();  // read by all before the next
+    if (x < 0) break;
+    int first = 0;
+    const int group = chunk_group(a, x, item, &first), er = group / a.Hkv, g = group - er * a.Hkv;
+    typedef const __attribute__((address_space(4))) ChunkEntry CE;  // scalar loads
+    CE *ep = (CE *)(a.entries + er);
+    ChunkEntry e{};
+    e.s = ep->s, e.ctx = ep->ctx, e.B = ep->B, e.qoff = ep->qoff;
+    e.nt = ep->nt, e.js = ep->js, e.np = ep->np, e.slot0 = ep->slot0;
+    const ChunkSeq seq{e.ctx, e.B, a.P, a.G, a.causal};
+    const int j = e.tile(item - first), piece = e.piece(item - first);
+    const int n = seq.keys(j);  // keys [0, n) are visible to some row
+    const int k0 = piece < 0 ? 0 : chunk_piece(n, e.np, piece), k1 = piece < 0 ? n : chunk_piece(n, e.np, piece + 1);
+    if (k0 >= k1) {  // uniform per workgroup
+      if (tid == 0) ahead = chunk_take(a, queue);
+      continue;
+    }
+    const int p0 = j * a.P, M = seq.rows(j);  // the tile's first position and its rows
+
+    // ---- query operands: element e of step st is dim st*16 + h*8 + e of row m ----
+    bf16x8 qop[NST];
+    const int m = wave * 32 + l32, mc = min(m, M - 1), mp = mc / a.G;  // rows past the tile: its last
+    const int lim = a.causal ? e.ctx + p0 + mp + 1 : n;            // keys the row sees
+    {
+      const char *qrow = (const char *)a.q + ((size_t)(e.qoff + p0 + mp) * a.Hq + g * a.G + (mc - mp * a.G)) * D * EB;
+#pragma unroll
+      for (int st = 0; st < NST; ++st) qop[st] = *(const bf16x8 *)(qrow + (st * 16 + h * 8) * EB);
+    }
+    const int vis_all = min(k1, a.causal ? e.ctx + p0 + min(wave * 32, M - 1) / a.G + 1 : n);  // keys that all its rows see
+    const bool act = wave * 32 < M;  // the wavefront has rows
+
+    f32x16 oacc[NDT];
+    float m_run = -INFINITY, l_run = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
+
+    // ---- key and value tiles: wavefronts 0-3 fetch rows 16w .. 16w + 15 of K, 4-7 those of V; they lie in one page ----
+    const int *table = a.block_table + (size_t)e.s * a.max_pages;
+    const bool isv = wave >= 4;
+    const int frow = (wave & 3) * 16;
+    const char *pool = (const char *)(isv ? a.v : a.k);
+    const int pmask = (1 << a.page_log2) - 1;
+    constexpr int RPI = 64 / T::CPR;  // rows of one load of a wavefront
+    const int lane_row = lane / T::CPR;
+    // The lane's vector of load i: row i * RPI + lane_row, whose swizzle differs from load 0's by 4i (K) or
+    // not at all (V).
+    const unsigned off0 = ((lane % T::CPR) ^ (isv ? T::swz_v(lane_row) : T::swz_k(lane_row))) * 16 + lane_row * T::ROWB;
+    const unsigned flip = isv ? 0 : 64;
+    auto page_of = [&](int t) __attribute__((always_inline)) {
+      const int kw = __builtin_amdgcn_readfirstlane(min(k0 + t * kChunkKT + frow, k1 - 1));
+      return ld_uniform(table, min(kw >> a.page_log2, a.max_pages - 1));
+    };
+    const unsigned lds0 = (unsigned)(uintptr_t)(char SDB_LDS *)(SDB_LDS void *)stages;
+    const char *src;  // of tile t: the wavefront's first row, in its page; rows past the last key re-read it (what
+    unsigned dst;     // lies behind it may hold anything), and a tile behind the last one is that key throughout
+    int most;         // the wavefront's last row that holds a key
+    auto start = [&](int t, int page_id) __attribute__((always_inline)) {
+      const int pg = min(max(page_id, 0), a.num_pages - 1), kw = k0 + t * kChunkKT + frow, last = k1 - 1;
+      most = max(last - kw, 0);
+      src = pool + ((((size_t)pg * a.Hkv + g) << a.page_log2) + (min(kw, last) & pmask)) * T::ROWB;
+      dst = lds0 + (t & 3) * T::STAGEB + (isv ? T::TILEB : 0) + frow * T::ROWB;
+    };
+    auto load = [&](int i) __attribute__((always_inline)) {
+      const int back = max(i * RPI + lane_row - most, 0);
+      chunk_load_lds(src, (off0 ^ (i * flip)) + i * 1024 - back * T::ROWB, dst + i * 1024);
+    };
+    // LDS addresses of the lane's operands in stage 0.  K: row l32, its 16-byte vectors 2 st + h.  V^T: lane l of
+    // a 16-lane group reads 4 dims of key row (l % 16) / 4 of four and receives, of dim 16 ((l / 16) % 2) +
+    // l % 16 of 32, those four keys.  Step st and dims dt only flip bits of the address.
+    const unsigned kaddr = lds0 + l32 * T::ROWB + ((h ^ T::swz_k(l32)) << 4);
+    const int vrow = 4 * h + ((lane & 15) >> 2);
+    const unsigned vaddr = lds0 + T::TILEB + vrow * T::ROWB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ T::swz_v(vrow)) << 4) +
+                           ((lane & 1) << 3);
+
+    const int nsteps = (k1 - k0 + kChunkKT - 1) / kChunkKT;
+    // ---- the products and the softmax of a step ----
+    f32x16 sacc[2];  // [kb]: register i is key kb*32 + 8*(i/4) + 4h + i%4 of row l32
+    bf16x8 pop[4];   // the weights of 16 keys each
+    // Products FROM .. TO - 1 of a step: NP of O^T += V^T P^T (tile t - 1), then those of S^T = K Q^T (tile t).
+    // Each product's left operand is read kAhead products before it; the order stays as written.
+    constexpr int NP = 4 * NDT, NPQ = NP + 2 * NST, kAhead = 6;
+    auto products = [&](auto from_c, auto to_c, int t, auto loads_c) __attribute__((always_inline)) {
+      constexpr int FROM = decltype(from_c)::value, TO = decltype(to_c)::value;
+      unsigned va = vaddr + ((t - 1) & 3) * T::STAGEB, ka = kaddr + (t & 3) * T::STAGEB;
+      asm("" : "+v"(va), "+v"(ka));  // the operands' addresses are made here, in the products' shadow, not kept in registers
+      bf16x8 op[NPQ];
+      auto read = [&](int i) __attribute__((always_inline)) {
+        if (i < NP) {
+          const int ks = i / NDT, dt = i % NDT;
+          s16x4c vv[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            vv[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (s16x4c SDB_LDS *)(uintptr_t)((va ^ (dt << 6)) + (ks * 16 + u * 8) * T::ROWB));
+          const s16x8c v8 = {vv[0][0], vv[0][1], vv[0][2], vv[0][3], vv[1][0], vv[1][1], vv[1][2], vv[1][3]};
+          op[i] = __builtin_bit_cast(bf16x8, v8);
+        } else {
+          const int st = (i - NP) / 2, kb = (i - NP) % 2;
+          op[i] = *(const bf16x8 SDB_LDS *)(uintptr_t)((ka ^ (st << 5)) + kb * 32 * T::ROWB);
+        }
+      };
+#pragma unroll
+      for (int i = FROM; i < FROM + kAhead; ++i) {
+        read(i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = FROM; i < TO; ++i) {
+        if (i < NP) {
+          oacc[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], pop[i / NDT], oacc[i % NDT], 0, 0, 0);
+        } else {
+          const int st = (i - NP) / 2, kb = (i - NP) % 2;
+          if (st == 0) {
+            f32x16 zero;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+            sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], qop[0], zero, 0, 0, 0);
+          } else {
+            sacc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i], qop[st], sacc[kb], 0, 0, 0);
+          }
+        }
+        if (i + kAhead < TO) read(i + kAhead);
+        if (decltype(loads_c)::value && i % 2 == 1 && i / 2 < T::NV) load(i / 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto softmax = [&](int kt) __attribute__((always_inline)) {
+      if (kt + kChunkKT > vis_all) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (kt + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= min(lim, k1)) sacc[kb][i] = -INFINITY;
+      }
+      float tmax = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (kt + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= lim) sacc[kb][i] = -INFINITY;
-    }
-    float tmax = -INFINITY;
+        for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sacc[kb][i]);
+      const float2 pm = pair_x32(tmax);
+      const float mt = fmaxf(pm.x, pm.y) * a.scale_log2;
+      if (__any(mt > m_run + kChunkLag)) {
+        const float mnew = fmaxf(m_run, mt);
+        const float alpha = mnew == -INFINITY ? 1.f : fast_exp2(m_run - mnew);
+        l_run *= alpha;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sacc[kb][i]);
-    const float2 pm = pair_x32(tmax);
-    const float mt = fmaxf(pm.x, pm.y) * a.scale_log2;
-    if (__any(mt > m_run + kChunkLag)) {
-      const float mnew = fmaxf(m_run, mt);
-      const float alpha = mnew == -INFINITY ? 1.f : fast_exp2(m_run - mnew);
-      l_run *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= alpha;
-      m_run = mnew;
-    }
-    const float muse = m_run == -INFINITY ? 0.f : m_run;
-    float psum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sacc[kb][i] = fast_exp2(fmaf(sacc[kb][i], a.scale_log2, -muse));
-        psum[kb] += sacc[kb][i];
+        for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= alpha;
+        m_run = mnew;
       }
-    l_run += psum[0] + psum[1];
+      const float muse = m_run == -INFINITY ? 0.f : m_run;
+      float psum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const f32x16 &p = sacc[ks >> 1];
-      const int i0 = 8 * (ks & 1);
-      const u32x4 raw{cvt_pk_bf16(p[i0], p[i0 + 1]), cvt_pk_bf16(p[i0 + 2], p[i0 + 3]),
-                      cvt_pk_bf16(p[i0 + 4], p[i0 + 5]), cvt_pk_bf16(p[i0 + 6], p[i0 + 7])};
-      const bf16x8 pop = __builtin_bit_cast(bf16x8, raw);
+      for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) {
-        s16x4c vv[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int r = ks * 16 + u * 8 + vrow;
-          const char *p8 = stage + T::TILEB + r * T::ROWB + (((4 * dt + vcol) ^ T::swz_v(r)) << 4) + ((lane & 1) << 3);
-          vv[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4c SDB_LDS *)p8);
+        for (int i = 0; i < 16; ++i) {
+          sacc[kb][i] = fast_exp2(fmaf(sacc[kb][i], a.scale_log2, -muse));
+          psum[kb] += sacc[kb][i];
         }
-        const s16x8c v8 = {vv[0][0], vv[0][1], vv[0][2], vv[0][3], vv[1][0], vv[1][1], vv[1][2], vv[1][3]};
-        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8), pop, oacc[dt], 0, 0, 0);
+      l_run += psum[0] + psum[1];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const f32x16 &p = sacc[ks >> 1];
+        const int i0 = 8 * (ks & 1);
+        const u32x4 raw{cvt_pk_bf16(p[i0], p[i0 + 1]), cvt_pk_bf16(p[i0 + 2], p[i0 + 3]),
+                        cvt_pk_bf16(p[i0 + 4], p[i0 + 5]), cvt_pk_bf16(p[i0 + 6], p[i0 + 7])};
+        pop[ks] = __builtin_bit_cast(bf16x8, raw);
       }
+    };
+
+    // ---- the steps ----
+    // The two wavefronts of a SIMD (w and w + 4) take turns at its matrix unit: in phase 2t the first four
+    // multiply P V of step t - 1 and Q K of step t while the others take the softmax of step t - 1, in
+    // phase 2t + 1 the first take the softmax of step t while the others multiply.  A barrier ends each
+    // phase.  A wavefront fetches its part of tile t + 2 while it multiplies, in phase 2t or 2t + 1, into the
+    // stage that was last read in phase 2t - 1; it has to be there for phase 2t + 4.
+    const bool second = wave >= 4;
+    auto load_all = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < T::NV; ++i) load(i);
+    };
+    {
+      const int id0 = page_of(0), id1 = page_of(1);
+      start(0, id0);
+      load_all();
+      start(1, id1);
+      load_all();
+    }
+    int id = page_of(2);
+#pragma unroll
+    for (int st = 0; st < NST; ++st) asm volatile("" : "+v"(qop[st]));  // waited for here, not in the loop
+    chunk_phase_end<T::NV>();                // tile 0 is here
+    if (second) chunk_phase_end<-1>();  // phase 0
+    start(2, id);
+    id = page_of(3);
+    load_all();
+    if (act) products(Int<NP>{}, Int<NPQ>{}, 0, Int<0>{});
+    auto between = [&]() __attribute__((always_inline)) {  // the products of a step and its softmax
+      if (second) chunk_phase_end<T::NV>();  // the next tile is here
+      else chunk_phase_end<-1>();
+    };
+    auto behind = [&]() __attribute__((always_inline)) {  // the softmax
+      if (second) chunk_phase_end<-1>();
+      else chunk_phase_end<T::NV>();
+    };
+    between();
+    if (act) softmax(k0);
+    behind();
+    for (int t = 1; t < nsteps; ++t) {
+      start(t + 2, id);
+      id = page_of(t + 3);
+      if (act) {
+        __builtin_amdgcn_s_setprio(1);
+        products(Int<0>{}, Int<NPQ>{}, t, Int<1>{});
+        __builtin_amdgcn_s_setprio(0);
+      } else {
+        load_all();
+      }
+      between();
+      if (act) softmax(k0 + t * kChunkKT);
+      behind();
+    }
+    if (tid == 0) ahead = chunk_take(a, queue);
+    if (act) products(Int<0>{}, Int<NP>{}, nsteps, Int<0>{});
+    chunk_phase_end<0>();  // no transfer is on its way, and (second) every wavefront is done with the tiles
+    if (!second) chunk_phase_end<-1>();
+
+    // ---- output: register i of oacc[dt] is dim dt*32 + 8*(i/4) + 4h + i%4 of row l32 ----
+    const float2 pl = pair_x32(l_run);
+    const float lsum = pl.x + pl.y;
+    if (m < M && piece < 0) {
+      const float inv = 1.f / lsum;
+      char *orow = (char *)a.out + ((size_t)(e.qoff + p0 + mp) * a.Hq + g * a.G + (m - mp * a.G)) * D * EB;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const f32x16 &o = oacc[dt];
+          *(uint2 *)(orow + (dt * 32 + c * 8 + h * 4) * EB) =
+              uint2{cvt_pk_bf16(o[4 * c] * inv, o[4 * c + 1] * inv), cvt_pk_bf16(o[4 * c + 2] * inv, o[4 * c + 3] * inv)};
+        }
+    } else if (m < M) {
+      // as the registers stand, so that a store is 1 KB in one place: vector (wave, dt, c, lane) of the slot
+      const size_t slot = e.slot(g, j, piece);
+      f32x4 *po = (f32x4 *)(a.part_o + slot * kChunkRows * D) + (wave * NDT * 4) * 64 + lane;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const f32x16 &o = oacc[dt];
+          __builtin_nontemporal_store(f32x4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]}, po + (dt * 4 + c) * 64);
+        }
+      if (h == 0) a.part_ml[slot * kChunkRows + m] = float2{m_run, lsum};
     }
   }
-
-  // ---- output: register i of oacc[dt] is dim dt*32 + 8*(i/4) + 4h + i%4 of row l32 ----
-  const float2 pl = pair_x32(l_run);
-  const float inv = 1.f / (pl.x + pl.y);
-  if (m >= M) return;
-  char *orow = (char *)a.out + ((size_t)(it.qoff + it.p0 + mp) * a.Hq + it.g * a.G + (m - mp * a.G)) * D * EB;
-#pragma unroll
-  for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const f32x16 &o = oacc[dt];
-      *(uint2 *)(orow + (dt * 32 + c * 8 + h * 4) * EB) =
-          uint2{cvt_pk_bf16(o[4 * c] * inv, o[4 * c + 1] * inv), cvt_pk_bf16(o[4 * c + 2] * inv, o[4 * c + 3] * inv)};
-    }
 }
+
+// Joins the pieces of the cut tiles:
+//   O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i,  M = max_i m_i
+// A workgroup takes the 32 rows that were one wavefront's, its four wavefronts a quarter of their vectors each.
+constexpr int kChunkMergeUnits = 8;  // of a tile
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
+  constexpr int NVEC = D / 8 / 4;  // vectors a lane joins
+  const int lane = threadIdx.x & 63, quarter = threadIdx.x >> 6, h = lane >> 5;
+  const int units = ld_uniform(&a.head->merges, 0) * kChunkMergeUnits;
+  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    const ChunkMerge t = a.merges[u / kChunkMergeUnits];
+    const int wave = u % kChunkMergeUnits, m = wave * 32 + (lane & 31);
+    if (m >= t.rows) continue;
+    const float2 *ml = a.part_ml + (size_t)t.slot * kChunkRows + m;
+    const f32x4 *po = (const f32x4 *)(a.part_o + (size_t)t.slot * kChunkRows * D) + (wave * (D / 8) + quarter * NVEC) * 64 + lane;
+    float mx = -INFINITY, lsum = 0.f;
+    f32x4 acc[NVEC];
+#pragma unroll
+    for (int v = 0; v < NVEC; ++v) acc[v] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+    for (int k = 0; k < t.np; ++k) {
+      if (chunk_piece(t.keys, t.np, k) >= chunk_piece(t.keys, t.np, k + 1)) continue;  // an empty piece
+      const float2 x = ml[(size_t)k * kChunkRows];
+      f32x4 o[NVEC];
+#pragma unroll
+      for (int v = 0; v < NVEC; ++v) o[v] = po[(size_t)k * (kChunkRows * D / 4) + v * 64];
+      if (x.x == -INFINITY) continue;  // a piece with no visible key
+      const float mn = fmaxf(mx, x.x), wo = mx == -INFINITY ? 0.f : fast_exp2(mx - mn), wn = fast_exp2(x.x - mn);
+      lsum = lsum * wo + x.y * wn;
+#pragma unroll
+      for (int v = 0; v < NVEC; ++v) acc[v] = acc[v] * wo + o[v] * wn;
+      mx = mn;
+    }
+    const float inv = 1.f / lsum;
+    const int mp = m / a.G;
+    char *orow = (char *)a.out + ((size_t)(t.row0 + mp) * a.Hq + t.g * a.G + (m - mp * a.G)) * D * 2;
+#pragma unroll
+    for (int v = 0; v < NVEC; ++v) {
+      const int i = quarter * NVEC + v;  // dt * 4 + c
+      *(uint2 *)(orow + ((i >> 2) * 32 + (i & 3) * 8 + h * 4) * 2) =
+          uint2{cvt_pk_bf16(acc[v][0] * inv, acc[v][1] * inv), cvt_pk_bf16(acc[v][2] * inv, acc[v][3] * inv)};
+    }
+  }
+}
+
+#endif  // __HIPCC__
 
 }  // namespace sdb

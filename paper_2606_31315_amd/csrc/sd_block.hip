@@ -686,7 +686,8 @@ namespace {
 struct ChunkPlan {
   bool block;             // small blocks: the block attention's kernels
   sd_attn_shape block_sh; // their shape
-  size_t total;   // workspace bytes
+  int slots, grid;        // pieces and workgroups at most
+  size_t off_entries, off_order, off_prefix, off_merges, off_ml, off_o, total;
 };
 
 int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
@@ -702,11 +703,25 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   const int G = sh->num_q_heads / sh->num_kv_heads;
   if (G > sdb::kChunkRows) return fail(SD_ERR_UNSUPPORTED, "group size %d exceeds %d", G, sdb::kChunkRows);
   if (!(sh->scale >= 0.f) || isinf(sh->scale)) return fail(SD_ERR_INVALID_ARG, "scale must be finite and >= 0");
-  const int P = sdb::kChunkRows / G;
-  if (((long long)sh->total_q / P + sh->num_seqs) * sh->num_kv_heads >= 1LL << 24)
-    return fail(SD_ERR_INVALID_ARG, "problem too large");
+  // Query tiles at most; the plan counts items in 32 bits and work in doubles.
+  const int P = sdb::kChunkRows / G, L = sh->max_kv_len;
+  const long long groups = (long long)sh->num_seqs * sh->num_kv_heads;
+  const long long tiles = ((long long)sh->total_q / P + sh->num_seqs) * sh->num_kv_heads;
+  const double units = (double)tiles * sdb::chunk_weight(sdb::kChunkRows) * ((double)L + sdb::kChunkPieceCost);
+  if (units >= 4503599627370496.0 || tiles > (1 << 30)) return fail(SD_ERR_INVALID_ARG, "problem too large");
   p->block = sh->max_block <= 64 && G * sh->max_block <= 256;
-  p->total = 256;
+  // Pieces: a tile of the longest ctx_s + B_s has no more than this many.
+  const long long longest = std::min<long long>(L, (long long)sh->max_ctx + sh->max_block);
+  const long long most = (longest + sdb::kChunkPieceCost + sdb::kChunkMinPiece - 1) / sdb::kChunkMinPiece;
+  p->slots = most > 1 ? (int)std::min<long long>(sdb::kChunkSlots, tiles * std::min<long long>(most, 64)) : 0;
+  p->grid = (int)std::max<long long>(1, std::min<long long>(sdb::kChunkGrid, tiles + p->slots));
+  p->off_entries = align256(sizeof(sdb::ChunkHead));
+  p->off_order = align256(p->off_entries + sizeof(sdb::ChunkEntry) * sh->num_seqs);
+  p->off_prefix = align256(p->off_order + sizeof(int) * sh->num_seqs);
+  p->off_merges = align256(p->off_prefix + sizeof(int) * sdb::kChunkQueues * ((groups + sdb::kChunkQueues - 1) / sdb::kChunkQueues));
+  p->off_ml = align256(p->off_merges + sizeof(sdb::ChunkMerge) * (p->slots / 2));
+  p->off_o = align256(p->off_ml + sizeof(float2) * sdb::kChunkRows * p->slots);
+  p->total = p->off_o + sizeof(float) * sdb::kChunkRows * sh->head_dim * p->slots;
   if (p->block) {
     // They are planned for the longest ctx_s + B_s, max_ctx + max_block; here max_kv_len bounds it too.
     p->block_sh = *sh;
@@ -773,9 +788,26 @@ int sd_chunk_attn_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_
   a.causal = mask_mode == SD_MASK_CAUSAL_IN_BLOCK;
   const float scale = sh->scale > 0.f ? sh->scale : 1.0f / sqrtf((float)sh->head_dim);
   a.scale_log2 = scale * 1.4426950408889634f;
-  const unsigned grid = (unsigned)((sh->total_q / a.P + sh->num_seqs) * sh->num_kv_heads);
-  if (sh->head_dim == 128) hipLaunchKernelGGL(sdb::chunk_attn_kernel<128>, dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(sdb::chunk_attn_kernel<64>, dim3(grid), dim3(512), 0, (hipStream_t)stream, a);
+  char *ws = (char *)workspace;
+  a.slots = p.slots;
+  a.grid = p.grid;
+  a.head = (sdb::ChunkHead *)ws;
+  a.entries = (sdb::ChunkEntry *)(ws + p.off_entries);
+  a.order = (int *)(ws + p.off_order);
+  a.prefix = (int *)(ws + p.off_prefix);
+  a.merges = (sdb::ChunkMerge *)(ws + p.off_merges);
+  a.part_ml = (float2 *)(ws + p.off_ml);
+  a.part_o = (float *)(ws + p.off_o);
+  hipStream_t st = (hipStream_t)stream;
+  hipLaunchKernelGGL(sdb::chunk_plan_kernel, dim3(1), dim3(sdb::kChunkPlanThreads), 0, st, a);
+  const int merge = p.slots / 2 * sdb::kChunkMergeUnits;  // units at most
+  if (sh->head_dim == 128) {
+    hipLaunchKernelGGL(sdb::chunk_attn_kernel<128>, dim3(p.grid), dim3(512), 0, st, a);
+    if (merge) hipLaunchKernelGGL(sdb::chunk_merge_kernel<128>, dim3(std::min(merge, 1024)), dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(sdb::chunk_attn_kernel<64>, dim3(p.grid), dim3(512), 0, st, a);
+    if (merge) hipLaunchKernelGGL(sdb::chunk_merge_kernel<64>, dim3(std::min(merge, 1024)), dim3(256), 0, st, a);
+  }
   return check_launch("sd_chunk_attn_paged");
 }
 
