@@ -443,15 +443,33 @@ def _norm_weight(w: Optional[torch.Tensor], name: str, like: torch.Tensor) -> No
         _need(w, name, like.dtype, like.device)
 
 
-def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
-                 inv_freq: Optional[torch.Tensor], *, q_weight: Optional[torch.Tensor] = None,
-                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
-                 rot_scale: float = 0.0, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
-                 stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
-    """Norm of every head of q [N, Hq, D] and k [N, Hkv, D] (where a weight [D] is given) and their rotation by
-    positions [N] int32 in one pass (sd_qk_norm_rope).  Rows may be strided (slices of a packed
-    projection); inv_freq [R/2] fp32 rotates the first R dims (None: none).  q or k may be None; an output
-    may be its input.  Returns (q_out, k_out)."""
+def _meta(t):
+    """All that the checks of a tensor look at: calls of tensors like those of an earlier one need not repeat them."""
+    if not isinstance(t, torch.Tensor):
+        return type(t)
+    return t.shape, t.stride(), t.dtype, t.get_device()
+
+
+def _on_current(dev: torch.device) -> None:
+    """The library launches on the current device."""
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _rope_pair(sh: SdRopeShape, x: Optional[torch.Tensor], w, out, which: str, dt, dev, N: int, D: int) -> None:
+    """The checks of q or k, its weight and its output (None: a new one), and their part of the shape."""
+    if x is None:
+        if out is not None or w is not None:
+            raise ValueError(f"an output or a weight is given for {which}, which is not")
+        return
+    stride, H = _rows(x, which, dt, dev, N, None, D), x.shape[1]
+    _norm_weight(w, which + "_weight", x)
+    setattr(sh, which + "_stride", stride)
+    setattr(sh, which + "_out_stride", 0 if out is None else _rows(out, which + "_out", dt, dev, N, H, D))
+    setattr(sh, "num_q_heads" if which == "q" else "num_kv_heads", H)
+
+
+def _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, rot_scale, q_out, k_out) -> SdRopeShape:
     x = q if q is not None else k
     if not isinstance(x, torch.Tensor):
         raise TypeError("q or k must be a torch.Tensor")
@@ -464,26 +482,63 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     if inv_freq is not None:
         _shape(inv_freq, "inv_freq", None)
         _need(inv_freq, "inv_freq", torch.float32, dev)
-    sh = SdRopeShape(0, N, 0, 0, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(bool(interleaved)),
+    sh = SdRopeShape(0, N, 0, 0, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved),
                      _dtype_code(x), float(eps), float(rot_scale))
-    if q is not None:
-        sh.q_stride, sh.num_q_heads = _rows(q, "q", dt, dev, N, None, D), q.shape[1]
-        _norm_weight(q_weight, "q_weight", q)
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=dev)
-        sh.q_out_stride = _rows(q_out, "q_out", dt, dev, N, q.shape[1], D)
-    if k is not None:
-        sh.k_stride, sh.num_kv_heads = _rows(k, "k", dt, dev, N, None, D), k.shape[1]
-        _norm_weight(k_weight, "k_weight", k)
-        if k_out is None:
-            k_out = torch.empty(k.shape, dtype=dt, device=dev)
-        sh.k_out_stride = _rows(k_out, "k_out", dt, dev, N, k.shape[1], D)
-    if (q is None and (q_out is not None or q_weight is not None)) or (
-            k is None and (k_out is not None or k_weight is not None)):
-        raise ValueError("an output or a weight is given for rows that are not")
-    _check(lib().sd_qk_norm_rope(ctypes.byref(sh), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq), _ptr(q_weight),
+    _rope_pair(sh, q, q_weight, q_out, "q", dt, dev, N, D)
+    _rope_pair(sh, k, k_weight, k_out, "k", dt, dev, N, D)
+    return sh
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+                 inv_freq: Optional[torch.Tensor], *, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                 rot_scale: float = 0.0, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Norm of every head of q [N, Hq, D] and k [N, Hkv, D] (where a weight [D] is given) and their rotation by
+    positions [N] int32 in one pass (sd_qk_norm_rope).  Rows may be strided (slices of a packed
+    projection); inv_freq [R/2] fp32 rotates the first R dims (None: none).  q or k may be None; an output
+    may be its input.  Returns (q_out, k_out)."""
+    interleaved = bool(interleaved)
+    key = ("rope", _meta(q), _meta(k), _meta(positions), _meta(inv_freq), _meta(q_weight), _meta(k_weight), eps,
+           interleaved, rot_scale, _meta(q_out), _meta(k_out))
+    c = _call_cache.get(key)
+    if c is None:
+        sh = _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, rot_scale, q_out, k_out)
+        c = _cached_call(key, lambda: sh, lambda _: 0)
+    _on_current(positions.device)
+    if q_out is None and q is not None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    _check(lib().sd_qk_norm_rope(c[1], _ptr(q), _ptr(k), positions.data_ptr(), _ptr(inv_freq), _ptr(q_weight),
                                  _ptr(k_weight), _ptr(q_out), _ptr(k_out), _stream(stream)))
     return q_out, k_out
+
+
+def _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight, k_weight, eps,
+                  interleaved, rot_scale, q_out) -> SdRopeShape:
+    _shape(k_pages, "k_pages", None, None, None, None)
+    _shape(v_pages, "v_pages", *k_pages.shape)
+    _, Hkv, _, D = k_pages.shape
+    dev, dt = k_pages.device, k_pages.dtype
+    _need(k_pages, "k_pages")
+    _need(v_pages, "v_pages", dt, dev)
+    ks = _rows(k_new, "k_new", dt, dev, None, Hkv, D)
+    N = k_new.shape[0]
+    vs = _rows(v_new, "v_new", dt, dev, N, Hkv, D)
+    _shape(block_table, "block_table", None, None)
+    S = block_table.shape[0]
+    _lens_shapes(S, ctx_lens=ctx_lens, q_offsets=q_offsets)
+    for name, t in (("block_table", block_table), ("ctx_lens", ctx_lens), ("q_offsets", q_offsets)):
+        _need(t, name, torch.int32, dev)
+    if inv_freq is not None:
+        _shape(inv_freq, "inv_freq", None)
+        _need(inv_freq, "inv_freq", torch.float32, dev)
+    _norm_weight(k_weight, "k_weight", k_new)
+    sh = SdRopeShape(S, N, 0, Hkv, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved),
+                     _dtype_code(k_pages), float(eps), float(rot_scale), 0, ks, vs)
+    _rope_pair(sh, q, q_weight, q_out, "q", dt, dev, N, D)
+    return sh
 
 
 def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, k_pages: torch.Tensor,
@@ -494,38 +549,23 @@ def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: 
                          q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
     """qk_norm_rope at positions ctx_s + i, with k and v written into page pools [num_pages, Hkv, page_size, D]
     through block_table [S, max_pages] (sd_kv_append_rope_paged).  q may be None (append only).  Returns q_out."""
-    _shape(k_pages, "k_pages", None, None, None, None)
-    _shape(v_pages, "v_pages", *k_pages.shape)
-    num_pages, Hkv, page_size, D = k_pages.shape
-    dev, dt = k_pages.device, k_pages.dtype
-    _need(k_pages, "k_pages")
-    _need(v_pages, "v_pages", dt, dev)
-    ks = _rows(k_new, "k_new", dt, dev, None, Hkv, D)
-    N = k_new.shape[0]
-    vs = _rows(v_new, "v_new", dt, dev, N, Hkv, D)
-    _shape(block_table, "block_table", None, None)
-    S, max_pages = block_table.shape
-    _lens_shapes(S, ctx_lens=ctx_lens, q_offsets=q_offsets)
-    for name, t in (("block_table", block_table), ("ctx_lens", ctx_lens), ("q_offsets", q_offsets)):
-        _need(t, name, torch.int32, dev)
-    if inv_freq is not None:
-        _shape(inv_freq, "inv_freq", None)
-        _need(inv_freq, "inv_freq", torch.float32, dev)
-    _norm_weight(k_weight, "k_weight", k_new)
-    sh = SdRopeShape(S, N, 0, Hkv, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(bool(interleaved)),
-                     _dtype_code(k_pages), float(eps), float(rot_scale), 0, ks, vs)
-    if q is not None:
-        sh.q_stride, sh.num_q_heads = _rows(q, "q", dt, dev, N, None, D), q.shape[1]
-        _norm_weight(q_weight, "q_weight", q)
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=dt, device=dev)
-        sh.q_out_stride = _rows(q_out, "q_out", dt, dev, N, q.shape[1], D)
-    elif q_out is not None or q_weight is not None:
-        raise ValueError("an output or a weight is given for rows that are not")
-    _check(lib().sd_kv_append_rope_paged(ctypes.byref(sh), page_size, num_pages, max_pages, _ptr(block_table), _ptr(q),
-                                         _ptr(k_new), _ptr(v_new), _ptr(ctx_lens), _ptr(q_offsets), _ptr(inv_freq),
-                                         _ptr(q_weight), _ptr(k_weight), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
-                                         _stream(stream)))
+    interleaved = bool(interleaved)
+    key = ("append", _meta(q), _meta(k_new), _meta(v_new), _meta(k_pages), _meta(v_pages), _meta(block_table),
+           _meta(ctx_lens), _meta(q_offsets), _meta(inv_freq), _meta(q_weight), _meta(k_weight), eps, interleaved,
+           rot_scale, _meta(q_out))
+    c = _call_cache.get(key)
+    if c is None:
+        sh = _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight,
+                           k_weight, eps, interleaved, rot_scale, q_out)
+        c = _cached_call(key, lambda: sh, lambda _: 0)
+    _on_current(k_pages.device)
+    if q_out is None and q is not None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    num_pages, _, page_size, _ = k_pages.shape
+    _check(lib().sd_kv_append_rope_paged(c[1], page_size, num_pages, block_table.shape[1], block_table.data_ptr(), _ptr(q),
+                                         k_new.data_ptr(), v_new.data_ptr(), ctx_lens.data_ptr(), q_offsets.data_ptr(),
+                                         _ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), _ptr(q_out),
+                                         k_pages.data_ptr(), v_pages.data_ptr(), _stream(stream)))
     return q_out
 
 
@@ -541,6 +581,29 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
     without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths."""
+    key = ("chunk", _meta(q), _meta(k_pages), _meta(v_pages), _meta(block_table), _meta(ctx_lens), _meta(chunk_lens),
+           _meta(q_offsets), int(max_ctx), int(max_chunk), float(scale), _meta(out))
+    c = _call_cache.get(key)
+    if c is None:
+        sh = _chunk_shape(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, max_ctx, max_chunk, scale, out)
+        c = _cached_call(key, lambda: sh, chunk_attn_workspace_size)
+    _, ref, nbytes = c
+    dev = q.device
+    _on_current(dev)
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = _default_ws.get(nbytes, dev)
+    num_pages, _, page_size, _ = k_pages.shape
+    _check(lib().sd_chunk_attn_paged(ref, page_size, num_pages, block_table.shape[1], block_table.data_ptr(), q.data_ptr(),
+                                     k_pages.data_ptr(), v_pages.data_ptr(), ctx_lens.data_ptr(), chunk_lens.data_ptr(),
+                                     q_offsets.data_ptr(), int(mask_mode), out.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def _chunk_shape(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, max_ctx, max_chunk, scale, out
+                 ) -> SdAttnShape:
     _shape(k_pages, "k_pages", None, None, None, None)
     _shape(v_pages, "v_pages", *k_pages.shape)
     _shape(q, "q", None, None, k_pages.shape[3])
@@ -554,23 +617,12 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     for name, t in (("block_table", block_table), ("ctx_lens", ctx_lens), ("chunk_lens", chunk_lens),
                     ("q_offsets", q_offsets)):
         _need(t, name, torch.int32, dev)
-    num_pages, Hkv, page_size, D = k_pages.shape
+    if out is not None:
+        _need(out, "out", q.dtype, dev)
+    _, Hkv, page_size, D = k_pages.shape
     S, max_pages = block_table.shape
-    if out is None:
-        out = torch.empty_like(q)
-    _need(out, "out", q.dtype, dev)
-    total_q, Hq, _ = q.shape
-    key = ("chunk", S, Hq, Hkv, D, max_pages, page_size, total_q, int(max_ctx), int(max_chunk), float(scale))
-    _, ref, nbytes = _cached_call(key, lambda: SdAttnShape(S, Hq, Hkv, D, max_pages * page_size, total_q, int(max_ctx),
-                                                           int(max_chunk), SD_BF16, float(scale)),
-                                  chunk_attn_workspace_size)
-    if workspace is None:
-        workspace = _default_ws.get(nbytes, dev)
-    _check(lib().sd_chunk_attn_paged(ref, page_size, num_pages, max_pages, _ptr(block_table), _ptr(q), _ptr(k_pages),
-                                     _ptr(v_pages), _ptr(ctx_lens), _ptr(chunk_lens), _ptr(q_offsets), int(mask_mode),
-                                     _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                     _stream(stream)))
-    return out
+    return SdAttnShape(S, q.shape[1], Hkv, D, max_pages * page_size, q.shape[0], int(max_ctx), int(max_chunk), SD_BF16,
+                       float(scale))
 
 
 def accept_shape(target_logits: torch.Tensor, num_seqs: int, max_block: int) -> SdAcceptShape:

@@ -35,7 +35,7 @@ constexpr int kChunkGrid = 256;       // workgroups at most: one fills a CU
 constexpr int kChunkSlots = 1024;     // pieces at most
 constexpr int kChunkSortSeqs = 4096;  // batches past this keep their order
 constexpr int kChunkPieceCost = 128;  // keys' worth of starting and ending an item
-constexpr int kChunkMinPiece = 256;   // keys of a piece at least
+constexpr int kChunkMinPiece = 512;   // keys of a piece at least
 constexpr int kChunkFew = 128;        // batches of less than this many tiles are cut throughout
 constexpr int kChunkSpread = 64;      // else a tile is cut where less than this many of its kind are left
 constexpr int kChunkEndPieces = 3;    // into this many pieces
@@ -56,7 +56,7 @@ struct ChunkSeq {
     return chunk_weight(P * G) * (n * each + (causal ? n * (n + 1) / 2 * P : 0));
   }
   SDB_HD double all_units() const { const int n = tiles(); return n ? before(n - 1) + units(n - 1) : 0; }
-  SDB_HD bool few() const { return B > 0 && B * G <= 64; }  // rows: bound by its keys' way from memory
+  SDB_HD bool few() const { return B > 0 && B <= 64 / G; }  // rows: bound by its keys' way from memory
   SDB_HD double longest() const {  // the last tile may have few rows
     const int n = tiles();
     const double u = n ? units(n - 1) : 0, v = n > 1 ? units(n - 2) : 0;

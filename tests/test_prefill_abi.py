@@ -137,7 +137,8 @@ def _t(*shape, dt=torch.bfloat16):
 
 def test_binding_refuses_wrong_shapes_and_host_tensors():
     q, k, pos, f = _t(5, 4, 128), _t(5, 2, 128), _t(5, dt=torch.int32), _t(64, dt=torch.float32)
-    for bad in (dict(q=_t(6, 4, 128)), dict(q=_t(5, 4, 64)), dict(positions=pos[:4]), dict(q=_t(5, 512)), dict(q=None, k=None)):
+    for bad in (dict(q=_t(6, 4, 128)), dict(q=_t(5, 4, 64)), dict(positions=pos[:4]), dict(q=_t(5, 512)), dict(q=None, k=None), dict(q=[1]), dict(positions=None),
+                dict(inv_freq=3.0), dict(q_weight=f), dict(k=None, k_out=k)):
         with pytest.raises((ValueError, TypeError)):
             L.qk_norm_rope(**{"q": q, "k": k, "positions": pos, "inv_freq": f, **bad})
     with pytest.raises(ValueError, match="device tensor"):
