@@ -346,6 +346,32 @@ __device__ __forceinline__ int chunk_group(const ChunkArgs &a, int x, int i, int
   return x + kChunkQueues * k;
 }
 
+// Tile b of the batch, sequences in order, within one the heads, within one the tiles: its sequence, head and number.
+__device__ __forceinline__ bool chunk_tile(const ChunkArgs &a, int b, ChunkEntry &e, int &g, int &j) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int c0 = 0; c0 < a.S; c0 += 64) {
+    const int k = min(c0 + lane, a.S - 1);  // clamped: no per-load branch
+    const int ctx = a.ctx_lens[k], B = a.chunk_lens[k], off = a.q_offsets[k];
+    const int nt = c0 + lane < a.S ? ChunkSeq{ctx, B, a.P, a.G, a.causal}.tiles() : 0;
+    const int items = nt * a.Hkv, incl = before + wave_scan_i(items);
+    const unsigned long long hit = __ballot(incl > b && incl - items <= b);
+    if (hit) {
+      const int l = __ffsll((long long)hit) - 1;  // wave-uniform
+      e.s = c0 + l;
+      e.ctx = __builtin_amdgcn_readlane(ctx, l);
+      e.B = __builtin_amdgcn_readlane(B, l);
+      e.qoff = __builtin_amdgcn_readlane(off, l);
+      const int n = __builtin_amdgcn_readlane(nt, l), r = b - __builtin_amdgcn_readlane(incl - items, l);
+      g = r / n;
+      j = r - g * n;
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
 // The running maximum may lag behind a row's scores by this much (log2 units) before the sums are
 // rescaled: weights then are at most 2^8 instead of 1, which changes no relative rounding, and the
 // rescaling of O, half as much work as the rest of the softmax, is left out of nearly every step.
@@ -370,46 +396,58 @@ __device__ __forceinline__ void chunk_phase_end() {
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-template <int D>
+template <int D, bool PLANNED>
 __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
   using T = ChunkTile<D>;
   constexpr int NST = D / 16, NDT = D / 32, EB = 2;
   __shared__ __attribute__((aligned(1024))) char stages[4 * T::STAGEB];  // a K and a V tile each
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  __shared__ int ticket[2];
   // Workgroups take the items of their XCD's queue, then those of the others.  Any may take any item: no result
   // depends on which.  The next item is asked for at the end of one.
+  __shared__ int ticket[2];
   int queue = blockIdx.x % kChunkQueues, ahead = blockIdx.x / kChunkQueues;
   for (;;) {  // one pass per item
-    if (tid == 0) {
-      while (ahead >= a.head->count[queue]) {
-        queue = chunk_other(a, queue);
-        if (queue < 0) break;
-        ahead = chunk_take(a, queue);
-      }
-      ticket[0] = queue;
-      ticket[1] = ahead;
-    }
-    __syncthreads();
-    const int x = __builtin_amdgcn_readfirstlane(ticket[0]), item = __builtin_amdgcn_readfirstlane(ticket[1]);
-    __syncthreads();  // read by all before the next
-    if (x < 0) break;
-    int first = 0;
-    const int group = chunk_group(a, x, item, &first), er = group / a.Hkv, g = group - er * a.Hkv;
-    typedef const __attribute__((address_space(4))) ChunkEntry CE;  // scalar loads
-    CE *ep = (CE *)(a.entries + er);
     ChunkEntry e{};
-    e.s = ep->s, e.ctx = ep->ctx, e.B = ep->B, e.qoff = ep->qoff;
-    e.nt = ep->nt, e.js = ep->js, e.np = ep->np, e.slot0 = ep->slot0;
-    const ChunkSeq seq{e.ctx, e.B, a.P, a.G, a.causal};
-    const int j = e.tile(item - first), piece = e.piece(item - first);
-    const int n = seq.keys(j);  // keys [0, n) are visible to some row
-    const int k0 = piece < 0 ? 0 : chunk_piece(n, e.np, piece), k1 = piece < 0 ? n : chunk_piece(n, e.np, piece + 1);
-    if (k0 >= k1) {  // uniform per workgroup
-      if (tid == 0) ahead = chunk_take(a, queue);
-      continue;
+    int g, j, piece, n, k0, k1;  // keys [0, n) are visible to some row; the item takes [k0, k1)
+    if constexpr (PLANNED) {
+      if (tid == 0) {
+        while (ahead >= a.head->count[queue]) {
+          queue = chunk_other(a, queue);
+          if (queue < 0) break;
+          ahead = chunk_take(a, queue);
+        }
+        ticket[0] = queue;
+        ticket[1] = ahead;
+      }
+      __syncthreads();
+      const int x = __builtin_amdgcn_readfirstlane(ticket[0]), item = __builtin_amdgcn_readfirstlane(ticket[1]);
+      __syncthreads();  // read by all before the next
+      if (x < 0) break;
+      int first = 0;
+      const int group = chunk_group(a, x, item, &first), er = group / a.Hkv;
+      g = group - er * a.Hkv;
+      typedef const __attribute__((address_space(4))) ChunkEntry CE;  // scalar loads
+      CE *ep = (CE *)(a.entries + er);
+      e.s = ep->s, e.ctx = ep->ctx, e.B = ep->B, e.qoff = ep->qoff;
+      e.nt = ep->nt, e.js = ep->js, e.np = ep->np, e.slot0 = ep->slot0;
+      j = e.tile(item - first);
+      piece = e.piece(item - first);
+      n = ChunkSeq{e.ctx, e.B, a.P, a.G, a.causal}.keys(j);
+      k0 = piece < 0 ? 0 : chunk_piece(n, e.np, piece);
+      k1 = piece < 0 ? n : chunk_piece(n, e.np, piece + 1);
+      if (k0 >= k1) {  // uniform per workgroup
+        if (tid == 0) ahead = chunk_take(a, queue);
+        continue;
+      }
+    } else {  // workgroup b takes whole tile b, if there is one
+      if (!chunk_tile(a, blockIdx.x, e, g, j)) break;
+      piece = -1;
+      n = ChunkSeq{e.ctx, e.B, a.P, a.G, a.causal}.keys(j);
+      k0 = 0;
+      k1 = n;
     }
+    const ChunkSeq seq{e.ctx, e.B, a.P, a.G, a.causal};
     const int p0 = j * a.P, M = seq.rows(j);  // the tile's first position and its rows
 
     // ---- query operands: element e of step st is dim st*16 + h*8 + e of row m ----
@@ -616,7 +654,9 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
       if (act) softmax(k0 + t * kChunkKT);
       behind();
     }
-    if (tid == 0) ahead = chunk_take(a, queue);
+    if constexpr (PLANNED) {
+      if (tid == 0) ahead = chunk_take(a, queue);
+    }
     if (act) products(Int<0>{}, Int<NP>{}, nsteps, Int<0>{});
     chunk_phase_end<0>();  // no transfer is on its way, and (second) every wavefront is done with the tiles
     if (!second) chunk_phase_end<-1>();
@@ -648,6 +688,7 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
         }
       if (h == 0) a.part_ml[slot * kChunkRows + m] = float2{m_run, lsum};
     }
+    if constexpr (!PLANNED) break;
   }
 }
 
