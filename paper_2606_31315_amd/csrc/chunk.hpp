@@ -5,7 +5,7 @@
 // to 256 rows, so a key row that a workgroup fetches serves all of them.  A workgroup of eight
 // wavefronts takes a tile, 32 rows a wavefront, and walks its keys 64 at a time:
 //   S^T = K Q^T    (32x32x16 bf16 matrix products, fp32 sums)
-//   P = exp2(S^T c - m), running row maximum m and row sum l in fp32
+//   P = exp2(S^T c - m), reference m near the running row maximum, row sum l in fp32
 //   O^T = O^T 2^(m_old - m) + V^T P^T   (P rounded to bf16 for the product; O^T fp32 in registers)
 // Scores come transposed, so a lane holds the scores of one query row (32 of a tile's 64 keys, its
 // partner lane the others) and the softmax needs one exchange between two lanes.  The weights then
@@ -372,10 +372,10 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs &a, int b, ChunkEntry
   return false;
 }
 
-// The running maximum may lag behind a row's scores by this much (log2 units) before the sums are
-// rescaled: weights then are at most 2^8 instead of 1, which changes no relative rounding, and the
-// rescaling of O, half as much work as the rest of the softmax, is left out of nearly every step.
-constexpr float kChunkLag = 8.f;
+// Weights are taken against the row's maximum when it was last looked for.  It is looked for again only
+// where a lane's 32 weights of a step sum to more than this: bf16 and fp32 hold such weights no less exactly,
+// and nearly every step does without the maximum, its exchange between lanes and the rescaling of O.
+constexpr float kChunkSum = 4096.f;
 
 // Fetches 16 bytes a lane from base + off to LDS bytes dst + 16 * lane.  As assembly without outputs: the
 // compiler knows of no transfer in flight and so makes no LDS read wait for all of them, as it does
@@ -567,39 +567,42 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
           for (int i = 0; i < 16; ++i)
             if (kt + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= min(lim, k1)) sacc[kb][i] = -INFINITY;
       }
-      float tmax = -INFINITY;
+      // The weights against a reference (log2 units), to the second product's operands; their sum.
+      auto weights = [&](float ref) __attribute__((always_inline)) {
+        float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+        for (int ks = 0; ks < 4; ++ks) {
+          uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sacc[kb][i]);
-      const float2 pm = pair_x32(tmax);
-      const float mt = fmaxf(pm.x, pm.y) * a.scale_log2;
-      if (__any(mt > m_run + kChunkLag)) {
-        const float mnew = fmaxf(m_run, mt);
+          for (int e = 0; e < 4; ++e) {
+            const f32x16 &sc = sacc[ks >> 1];
+            const int i = 8 * (ks & 1) + 2 * e;
+            const float x = fast_exp2(fmaf(sc[i], a.scale_log2, -ref)), y = fast_exp2(fmaf(sc[i + 1], a.scale_log2, -ref));
+            w[e] = cvt_pk_bf16(x, y);
+            sum[0] += x;
+            sum[1] += y;
+          }
+          pop[ks] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+        }
+        return sum[0] + sum[1];
+      };
+      float sum = weights(m_run);
+      if (__any(!(sum <= kChunkSum))) {  // also before the first key (the reference is -inf) and where a sum is no number
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sacc[kb][i]);
+        const float2 pm = pair_x32(tmax);
+        const float mnew = fmaxf(m_run, fmaxf(pm.x, pm.y) * a.scale_log2);
         const float alpha = mnew == -INFINITY ? 1.f : fast_exp2(m_run - mnew);
         l_run *= alpha;
 #pragma unroll
         for (int dt = 0; dt < NDT; ++dt) oacc[dt] *= alpha;
         m_run = mnew;
+        sum = weights(mnew == -INFINITY ? 0.f : mnew);
       }
-      const float muse = m_run == -INFINITY ? 0.f : m_run;
-      float psum[2] = {0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          sacc[kb][i] = fast_exp2(fmaf(sacc[kb][i], a.scale_log2, -muse));
-          psum[kb] += sacc[kb][i];
-        }
-      l_run += psum[0] + psum[1];
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const f32x16 &p = sacc[ks >> 1];
-        const int i0 = 8 * (ks & 1);
-        const u32x4 raw{cvt_pk_bf16(p[i0], p[i0 + 1]), cvt_pk_bf16(p[i0 + 2], p[i0 + 3]),
-                        cvt_pk_bf16(p[i0 + 4], p[i0 + 5]), cvt_pk_bf16(p[i0 + 6], p[i0 + 7])};
-        pop[ks] = __builtin_bit_cast(bf16x8, raw);
-      }
+      l_run += sum;
     };
 
     // ---- the steps ----
