@@ -33,7 +33,7 @@ constexpr int kChunkKT = 64;     // keys of a step
 constexpr int kChunkQueues = 8;
 constexpr int kChunkGrid = 256;       // workgroups at most: one fills a CU
 constexpr int kChunkSlots = 1024;     // pieces at most
-constexpr int kChunkSortSeqs = 4096;  // batches past this keep their order
+constexpr int kChunkSortSeqs = 1024;  // batches past this keep their order
 constexpr int kChunkPieceCost = 128;  // keys' worth of starting and ending an item
 constexpr int kChunkMinPiece = 512;   // keys of a piece at least
 constexpr int kChunkFew = 128;        // batches of less than this many tiles are cut throughout
@@ -72,8 +72,7 @@ struct ChunkSplit {
 SDB_HD ChunkSplit chunk_split(const ChunkSeq &q, int Hkv, double after, double total) {
   const int nt = q.tiles();
   int lo = 0, hi = nt;
-  while (lo < hi) {  // the first js that is not cut (a search, as if there were one)
-    const int j = lo + (hi - lo) / 2;
+  for (int j = nt - 1; lo < hi; j = lo + (hi - lo) / 2) {  // the first tile that is not cut (a search, as if there were one)
     if (total < kChunkFew * q.units(j) || after + Hkv * (q.before(j) + q.units(j)) < kChunkSpread * q.units(j)) lo = j + 1;
     else hi = j;
   }
@@ -159,7 +158,6 @@ struct ChunkArgs {
   // workspace
   ChunkHead *head;
   ChunkEntry *entries;       // [S]
-  int *order;                // [S] the plan's own
   int *prefix;               // [8, ceil(S Hkv / 8)] first item of each group of a queue
   ChunkMerge *merges;        // [slots / 2]
   float *part_o;             // [slots, 256, D] unnormalised sums
@@ -186,23 +184,24 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs &a, int s) {
 // The plan, by one workgroup.  Sums of work are whole numbers in doubles and every order is fixed: the same lengths
 // give the same plan.
 constexpr int kChunkPlanThreads = 1024;
+static_assert(kChunkSortSeqs <= kChunkPlanThreads, "a thread per sequence");
 __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   __shared__ float key[kChunkSortSeqs], place[kChunkSortSeqs];
+  __shared__ int order[kChunkSortSeqs], items[kChunkSortSeqs];
   __shared__ double sums[kChunkPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.S;
   const bool sorted = S <= kChunkSortSeqs;
   // the batch's work; sequences by their longest tile, those of few rows marked by the sign
   double mine = 0;
+  float k = 0.f, work = 0.f;
   for (int s = tid; s < S; s += kChunkPlanThreads) {
     const ChunkSeq q = chunk_seq(a, s);
-    mine += q.all_units() * a.Hkv;
-    if (sorted) {
-      key[s] = (float)q.longest() * (q.few() ? -1.f : 1.f);
-      place[s] = (float)q.all_units();
-    } else {
-      a.order[s] = s;
-    }
+    const double u = q.all_units();
+    mine += u * a.Hkv;
+    k = (float)q.longest() * (q.few() ? -1.f : 1.f);
+    work = (float)u;
   }
+  if (tid < kChunkSortSeqs) key[tid] = k, place[tid] = work;
   mine = wave_sum_d(mine);
   if (lane == 0) sums[wave] = mine;
   __syncthreads();
@@ -210,34 +209,26 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
   for (int w = 0; w < kChunkPlanThreads / 64; ++w) total += sums[w];
   if (sorted) {
     // Each kind longest first, and the two interleaved by the share of their work that is done by then.
-    float at[kChunkSortSeqs / kChunkPlanThreads];
-#pragma unroll
-    for (int i = 0; i < kChunkSortSeqs / kChunkPlanThreads; ++i) {
-      const int s = tid + i * kChunkPlanThreads;
-      if (s >= S) break;
-      const float k = key[s];
-      float before = 0.f, all = 0.f;
+    float before = 0.f, all = 0.f;
+    if (tid < S) {
+#pragma unroll 4
       for (int t = 0; t < S; ++t) {
-        const float u = key[t], w = place[t];
-        const bool same = (u < 0.f) == (k < 0.f);
-        all += same ? w : 0.f;
-        before += same && (fabsf(u) > fabsf(k) || (u == k && t < s)) ? w : 0.f;
+        const float u = key[t], w = (u < 0.f) == (k < 0.f) ? place[t] : 0.f;
+        all += w;
+        before += fabsf(u) > fabsf(k) || (u == k && t < tid) ? w : 0.f;
       }
-      at[i] = all > 0.f ? (before + 0.5f * place[s]) / all : 2.f;  // sequences without rows come last
     }
+    const float at = all > 0.f ? (before + 0.5f * work) / all : 2.f;  // sequences without rows come last
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kChunkSortSeqs / kChunkPlanThreads; ++i)
-      if (tid + i * kChunkPlanThreads < S) place[tid + i * kChunkPlanThreads] = at[i];
+    if (tid < S) place[tid] = at;
     __syncthreads();
-    for (int s = tid; s < S; s += kChunkPlanThreads) {
-      const float k = place[s];
+    if (tid < S) {
       int rank = 0;
-      for (int t = 0; t < S; ++t) rank += place[t] < k || (place[t] == k && t < s);
-      a.order[rank] = s;
+#pragma unroll 4
+      for (int t = 0; t < S; ++t) rank += place[t] < at || (place[t] == at && t < tid);
+      order[rank] = tid;
     }
   }
-  __threadfence_block();
   __syncthreads();
   // entries from the last to the first, 64 a round: what lies behind each is known then
   if (wave == 0) {
@@ -247,7 +238,7 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
       const int r = min(c0 + lane, S - 1);
       const bool live = c0 + lane < S;
       ChunkEntry e{};
-      e.s = a.order[r];
+      e.s = sorted ? order[r] : r;
       const ChunkSeq q = chunk_seq(a, e.s);
       e.ctx = q.ctx;
       e.B = q.B;
@@ -265,7 +256,10 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
       e.items = e.nt - sp.js + sp.js * sp.np;
       const int mi = wave_scan_i(sp.js * a.Hkv), mall = __builtin_amdgcn_readlane(mi, 63);
       e.merge0 = merges + mall - mi;
-      if (live) a.entries[r] = e;
+      if (live) {
+        a.entries[r] = e;
+        if (sorted) items[r] = e.items;
+      }
       after += all;
       slots += wall;
       merges += mall;
@@ -279,23 +273,25 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
     int base = 0;
     for (int k0 = 0; k0 < n; k0 += 64) {
       const int k = min(k0 + lane, n - 1);
-      const int items = k0 + lane < n ? a.entries[(x + kChunkQueues * k) / a.Hkv].items : 0;
-      const int incl = wave_scan_i(items);
-      if (k0 + lane < n) a.prefix[x * stride + k] = base + incl - items;
+      const int r = (x + kChunkQueues * k) / a.Hkv, m = k0 + lane < n ? (sorted ? items[r] : a.entries[r].items) : 0;
+      const int incl = wave_scan_i(m);
+      if (k0 + lane < n) a.prefix[x * stride + k] = base + incl - m;
       base += __builtin_amdgcn_readlane(incl, 63);
     }
     if (lane == 0) {
       a.head->next[x].v = ((int)a.grid - x + kChunkQueues - 1) / kChunkQueues;  // each workgroup's first item is its own
       a.head->count[x] = base;
     }
-  } else {  // the list of cut tiles, the sequences that have some in turn
-    const int t0 = tid - kChunkQueues * 64, nt0 = kChunkPlanThreads - kChunkQueues * 64;
+  } else {  // the list of cut tiles: the sequences that have some go round the other wavefronts
+    int turn = wave;
+    constexpr int kTurns = kChunkPlanThreads / 64 - kChunkQueues;
     for (int c0 = 0; c0 < S; c0 += 64) {
       const ChunkEntry e = a.entries[min(c0 + lane, S - 1)];
       unsigned long long cut = __ballot(c0 + lane < S && e.js > 0);
       while (cut) {
         const int l = __ffsll((long long)cut) - 1;
         cut &= cut - 1;
+        if (turn++ % kTurns) continue;
         ChunkEntry u{};
         u.ctx = __builtin_amdgcn_readlane(e.ctx, l);
         u.B = __builtin_amdgcn_readlane(e.B, l);
@@ -305,7 +301,7 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
         u.slot0 = __builtin_amdgcn_readlane(e.slot0, l);
         u.merge0 = __builtin_amdgcn_readlane(e.merge0, l);
         const ChunkSeq q{u.ctx, u.B, a.P, a.G, a.causal};
-        for (int t = t0; t < u.js * a.Hkv; t += nt0) {
+        for (int t = lane; t < u.js * a.Hkv; t += 64) {
           const int g = t / u.js, j = t - g * u.js;
           a.merges[u.merge0 + t] = ChunkMerge{u.qoff + j * a.P, g, q.rows(j), q.keys(j), u.np, u.slot(g, j, 0), {0, 0}};
         }

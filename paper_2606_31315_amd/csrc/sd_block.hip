@@ -688,7 +688,7 @@ struct ChunkPlan {
   sd_attn_shape block_sh; // their shape
   bool direct;            // few short tiles: one launch, a workgroup per tile
   int slots, grid;        // pieces and workgroups at most
-  size_t off_entries, off_order, off_prefix, off_merges, off_ml, off_o, total;
+  size_t off_entries, off_prefix, off_merges, off_ml, off_o, total;
 };
 
 int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
@@ -723,8 +723,7 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   p->direct = tiles <= sdb::kChunkGrid && (longest + sdb::kChunkKT - 1) / sdb::kChunkKT * (np - 1) <= 16 * np;
   if (p->direct) p->slots = 0, p->grid = (int)std::max<long long>(1, tiles);
   p->off_entries = align256(sizeof(sdb::ChunkHead));
-  p->off_order = align256(p->off_entries + sizeof(sdb::ChunkEntry) * sh->num_seqs);
-  p->off_prefix = align256(p->off_order + sizeof(int) * sh->num_seqs);
+  p->off_prefix = align256(p->off_entries + sizeof(sdb::ChunkEntry) * sh->num_seqs);
   p->off_merges = align256(p->off_prefix + sizeof(int) * sdb::kChunkQueues * ((groups + sdb::kChunkQueues - 1) / sdb::kChunkQueues));
   p->off_ml = align256(p->off_merges + sizeof(sdb::ChunkMerge) * (p->slots / 2));
   p->off_o = align256(p->off_ml + sizeof(float2) * sdb::kChunkRows * p->slots);
@@ -800,7 +799,6 @@ int sd_chunk_attn_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_
   a.grid = p.grid;
   a.head = (sdb::ChunkHead *)ws;
   a.entries = (sdb::ChunkEntry *)(ws + p.off_entries);
-  a.order = (int *)(ws + p.off_order);
   a.prefix = (int *)(ws + p.off_prefix);
   a.merges = (sdb::ChunkMerge *)(ws + p.off_merges);
   a.part_ml = (float2 *)(ws + p.off_ml);
