@@ -239,6 +239,27 @@ class Workspace:
 _default_ws = Workspace()
 
 
+class StreamWorkspace:
+    """A device scratch buffer per stream, grown on demand: calls on one stream are ordered, and a buffer
+    that is grown out of goes back to the allocator behind its own stream's work."""
+
+    def __init__(self):
+        self._bufs = {}
+
+    def get(self, nbytes: int, device: torch.device, stream) -> torch.Tensor:
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("give a workspace in a call that is captured: the graph keeps its address")
+        key = (device.index, _stream(stream))
+        buf = self._bufs.get(key)
+        if buf is None or buf.numel() < nbytes:
+            with torch.cuda.stream(stream):  # None: the current one
+                buf = self._bufs[key] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+        return buf
+
+
+_stream_ws = StreamWorkspace()
+
+
 def attn_shape(q: torch.Tensor, k_cache: torch.Tensor, max_ctx: int, max_block: int, scale: float = 0.0
                ) -> SdAttnShape:
     S, Hkv, Lmax, D = k_cache.shape
@@ -580,7 +601,8 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      max_ctx: int, max_chunk: int, scale: float = 0.0, out: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
-    without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths."""
+    without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  Without a
+    workspace a buffer of the stream's is used; a captured call needs its own."""
     key = ("chunk", _meta(q), _meta(k_pages), _meta(v_pages), _meta(block_table), _meta(ctx_lens), _meta(chunk_lens),
            _meta(q_offsets), int(max_ctx), int(max_chunk), float(scale), _meta(out))
     c = _call_cache.get(key)
@@ -593,7 +615,7 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     if out is None:
         out = torch.empty_like(q)
     if workspace is None:
-        workspace = _default_ws.get(nbytes, dev)
+        workspace = _stream_ws.get(nbytes, dev, stream)
     num_pages, _, page_size, _ = k_pages.shape
     _check(lib().sd_chunk_attn_paged(ref, page_size, num_pages, block_table.shape[1], block_table.data_ptr(), q.data_ptr(),
                                      k_pages.data_ptr(), v_pages.data_ptr(), ctx_lens.data_ptr(), chunk_lens.data_ptr(),

@@ -187,3 +187,60 @@ def test_empty_calls():
     out = torch.full_like(b["q"], 3.0)
     b["B"], b["off"] = b["B"] * 0, b["off"] * 0
     assert bool((_run(b, CAUSAL, out=out, max_chunk=80) == 3.0).all())
+
+
+def test_capture_needs_a_workspace():
+    b = R.chunk_batch(93, 16, 8, 128, 16, [10], [80], G.dev())
+    ctx, B, off = _i32(b["ctx"]), _i32(b["B"]), _i32(b["off"])
+    out = torch.empty_like(b["q"])
+    x = torch.zeros(1, device=G.dev())
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x.add_(1)
+        with pytest.raises(ValueError, match="workspace"):
+            sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], ctx, B, off, CAUSAL, max_ctx=10, max_chunk=80, out=out)
+
+
+def test_two_streams_at_once_without_workspaces():
+    """Calls on two streams that run at the same time, growing their buffers: each as alone."""
+    batches = [R.chunk_batch(101 + i, 32, 8, 128, 64, [2000 + 900 * i, 0, 64], [150 + 70 * i, 200, 1], G.dev()) for i in range(4)]
+    refs = [_run(b, CAUSAL) for b in batches]
+    lens = [[_i32(b[x]) for x in ("ctx", "B", "off")] for b in batches]
+    outs = [torch.zeros_like(b["q"]) for b in batches]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    G.log("sd_chunk_attn_paged on two streams at once")
+    for i, (b, l, o) in enumerate(zip(batches, lens, outs)):
+        sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], *l, CAUSAL, max_ctx=int(b["ctx"].max()),
+                            max_chunk=int(b["B"].max()), out=o, stream=streams[i % 2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, r) for o, r in zip(outs, refs))
+
+
+@pytest.mark.parametrize("S", [1025, 1500], ids=["just_past", "well_past"])
+def test_more_sequences_than_the_plan_orders(S):
+    """Batches past the plan's sorting, most of them single rows, on the planned path."""
+    rng = np.random.default_rng(S)
+    B = np.where(rng.random(S) < 0.05, rng.integers(60, 100, S), rng.integers(0, 3, S))
+    B[[3, 1024]] = [300, 77]
+    _check(R.chunk_batch(S, 8, 2, 64, 16, rng.integers(0, 60, S), B, G.dev()), CAUSAL)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_cut_tiles_over_long_contexts(D):
+    """Tiles cut into many pieces, rows that see nothing of the last ones, short sequences beside them."""
+    _check(R.chunk_batch(111 + D, 8, 2, D, 64, [20000, 0, 333], [100, 65, 1], G.dev()), CAUSAL)
+    _check(R.chunk_batch(112 + D, 4, 4, D, 64, [0], [2500], G.dev()), CAUSAL)
+
+
+def test_whole_batches_of_every_path_agree_with_their_chunks():
+    """One prompt in one chunk and in uneven chunks: each within its tolerance of the plain form."""
+    b = R.chunk_batch(121, 16, 4, 128, 64, [0], [900], G.dev())
+    _check(b, CAUSAL)
+    done = 0
+    for n in (1, 64, 65, 300, 470):
+        c = dict(b, q=b["q"][done:done + n].contiguous(), ctx=np.array([done], np.int32), B=np.array([n], np.int32),
+                 off=np.array([0, n], np.int32))
+        _check(c, CAUSAL)
+        done += n
+    assert done == 900

@@ -263,3 +263,16 @@ def test_graph_replays():
         ctx += 1
         q.mul_(1.5), k.mul_(-0.75), v.add_(1.0)
         torch.cuda.synchronize()
+
+
+def test_more_rows_than_workgroups():
+    """4.3 million rows of one head: the grid ends at 2^20 workgroups, which go round."""
+    N = 4_300_000
+    q = torch.randn(N, 1, 64, dtype=BF, device=G.dev())
+    pos = torch.arange(N, dtype=torch.int32, device=G.dev())
+    f = _inv_freq(64)
+    G.log(f"sd_qk_norm_rope N={N}")
+    o, _ = sd.qk_norm_rope(q, None, pos, f)
+    torch.cuda.synchronize()
+    for lo in (0, (1 << 22) - 8, N - 16):
+        R.assert_turned(o[lo:lo + 16], *R.turned(q[lo:lo + 16], None, pos[lo:lo + 16], f))

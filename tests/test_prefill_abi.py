@@ -170,3 +170,16 @@ def test_row_strides():
         rows(x[:1, :512].expand(6, 512).unflatten(1, (4, 128)), 4)
     with pytest.raises(TypeError):
         rows(x[:, :512].unflatten(1, (4, 128)), 4, torch.float32)
+
+
+def test_binding_takes_meta_tensors_to_the_device_check():
+    """Right shapes without memory stop at the device check, in every call."""
+    m = lambda *s, dt=torch.bfloat16: torch.empty(*s, dtype=dt, device="meta")  # noqa: E731
+    i = lambda *s: m(*s, dt=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="device tensor"):
+        L.qk_norm_rope(m(5, 4, 128), m(5, 2, 128), i(5), m(64, dt=torch.float32))
+    with pytest.raises(ValueError, match="device tensor"):
+        L.kv_append_rope_paged(m(5, 4, 128), m(5, 2, 128), m(5, 2, 128), m(9, 2, 16, 128), m(9, 2, 16, 128), i(3, 4), i(3),
+                               i(4), m(64, dt=torch.float32))
+    with pytest.raises(ValueError, match="device tensor"):
+        L.chunk_attn_paged(m(5, 4, 128), m(9, 2, 16, 128), m(9, 2, 16, 128), i(3, 4), i(3), i(3), i(4), 0, max_ctx=0, max_chunk=5)
