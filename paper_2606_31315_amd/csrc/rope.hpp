@@ -31,6 +31,7 @@ struct RopeArgs {
   int total_q, Hq, Hkv, rot, interleaved;
   float eps, rot_scale;
   int groups;                // wavefronts a token's heads take
+  int once;                  // rows are loaded past the caches
   // paged call
   void *k_pages, *v_pages;   // [num_pages, Hkv, page_size, D]
   const int *ctx_lens, *q_offsets, *block_table;
@@ -45,6 +46,13 @@ struct Vec8 {
   __device__ __forceinline__ void load(const char *p) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) raw[i] = reinterpret_cast<const u32x4 *>(p)[i];
+  }
+  __device__ __forceinline__ void load_once(const char *p) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const v4u32 v = __builtin_nontemporal_load(reinterpret_cast<const v4u32 *>(p) + i);
+      raw[i] = u32x4{v[0], v[1], v[2], v[3]};
+    }
   }
   __device__ __forceinline__ void store(char *p) const {
 #pragma unroll
@@ -104,7 +112,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                       : kv == 1 ? (const char *)a.k + ((long long)r * a.k_stride + h * D) * EB
                                 : (const char *)a.v + ((long long)r * a.v_stride + h * D) * EB;
     Vec8<BF16> v0, v1;
-    if (live) {
+    if (live && a.once) {
+      v0.load_once(src + d0 * EB);
+      v1.load_once(src + d1 * EB);
+    } else if (live) {
       v0.load(src + d0 * EB);
       v1.load(src + d1 * EB);
     }
