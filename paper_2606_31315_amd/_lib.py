@@ -471,10 +471,11 @@ def _meta(t):
     return t.shape, t.stride(), t.dtype, t.get_device()
 
 
-def _on_current(dev: torch.device) -> None:
+def _on_current(t: torch.Tensor) -> None:
     """The library launches on the current device."""
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    cur = _cur_device() if _cur_device is not None else torch.cuda.current_device()
+    if t.get_device() != cur:
+        raise ValueError(f"the tensors are on {t.device}, the current device is cuda:{cur}")
 
 
 def _rope_pair(sh: SdRopeShape, x: Optional[torch.Tensor], w, out, which: str, dt, dev, N: int, D: int) -> None:
@@ -526,7 +527,7 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     if c is None:
         sh = _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, rot_scale, q_out, k_out)
         c = _cached_call(key, lambda: sh, lambda _: 0)
-    _on_current(positions.device)
+    _on_current(positions)
     if q_out is None and q is not None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if k_out is None and k is not None:
@@ -579,7 +580,7 @@ def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: 
         sh = _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight,
                            k_weight, eps, interleaved, rot_scale, q_out)
         c = _cached_call(key, lambda: sh, lambda _: 0)
-    _on_current(k_pages.device)
+    _on_current(k_pages)
     if q_out is None and q is not None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     num_pages, _, page_size, _ = k_pages.shape
@@ -610,12 +611,11 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
         sh = _chunk_shape(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, max_ctx, max_chunk, scale, out)
         c = _cached_call(key, lambda: sh, chunk_attn_workspace_size)
     _, ref, nbytes = c
-    dev = q.device
-    _on_current(dev)
+    _on_current(q)
     if out is None:
         out = torch.empty_like(q)
     if workspace is None:
-        workspace = _stream_ws.get(nbytes, dev, stream)
+        workspace = _stream_ws.get(nbytes, q.device, stream)
     num_pages, _, page_size, _ = k_pages.shape
     _check(lib().sd_chunk_attn_paged(ref, page_size, num_pages, block_table.shape[1], block_table.data_ptr(), q.data_ptr(),
                                      k_pages.data_ptr(), v_pages.data_ptr(), ctx_lens.data_ptr(), chunk_lens.data_ptr(),

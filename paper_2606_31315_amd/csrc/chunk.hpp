@@ -325,12 +325,11 @@ __device__ __forceinline__ int chunk_take(const ChunkArgs &a, int x) {
   return __hip_atomic_fetch_add(&a.head->next[x].v, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The group of queue x that holds item i: the last whose first item is at most i.
-__device__ __forceinline__ int chunk_group(const ChunkArgs &a, int x, int i, int *first) {
+// The group of queue x that holds item i: the last whose first item is at most i.  k: where to look from, and its place.
+__device__ __forceinline__ int chunk_group(const ChunkArgs &a, int x, int i, int &k, int *first) {
   const int lane = threadIdx.x & 63;
   const int n = chunk_groups((long long)a.S * a.Hkv, x), stride = (a.S * a.Hkv + kChunkQueues - 1) / kChunkQueues;
-  int k = 0;
-  for (int k0 = 0; k0 < n; k0 += 64) {
+  for (int k0 = k & ~63; k0 < n; k0 += 64) {
     const int p = a.prefix[x * stride + min(k0 + lane, n - 1)];
     const unsigned long long le = __ballot(k0 + lane < n && p <= i);
     if (!le) break;
@@ -405,6 +404,7 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
   // depends on which.  The next item is asked for at the end of one.
   __shared__ int ticket[2];
   int queue = blockIdx.x % kChunkQueues, ahead = blockIdx.x / kChunkQueues;
+  [[maybe_unused]] int looked = -1, place = 0;
   for (;;) {  // one pass per item
     ChunkEntry e{};
     int g, j, piece, n, k0, k1;  // keys [0, n) are visible to some row; the item takes [k0, k1)
@@ -422,8 +422,10 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
       const int x = __builtin_amdgcn_readfirstlane(ticket[0]), item = __builtin_amdgcn_readfirstlane(ticket[1]);
       __syncthreads();  // read by all before the next
       if (x < 0) break;
+      if (x != looked) place = 0;  // a queue's items come in order
+      looked = x;
       int first = 0;
-      const int group = chunk_group(a, x, item, &first), er = group / a.Hkv;
+      const int group = chunk_group(a, x, item, place, &first), er = group / a.Hkv;
       g = group - er * a.Hkv;
       typedef const __attribute__((address_space(4))) ChunkEntry CE;  // scalar loads
       CE *ep = (CE *)(a.entries + er);

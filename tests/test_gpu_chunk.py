@@ -86,17 +86,18 @@ def test_growing_scores():
     _check(b, CAUSAL, scale=0.05)
 
 
-def test_loose_bounds_and_padding():
+@pytest.mark.parametrize("rows,max_chunk", [((100, 71), 5000), ((40, 1), 64)], ids=["chunk_kernel", "block_kernels"])
+def test_loose_bounds_and_padding(rows, max_chunk):
     """Bounds far above the lengths, a batch padded with rows and sequences: rows behind the last sequence
     stay as they were."""
-    b = R.chunk_batch(31, 32, 8, 128, 16, [300, 0, 40, 0], [100, 0, 71, 0], G.dev())
+    b = R.chunk_batch(31, 32, 8, 128, 16, [300, 0, 40, 0], [rows[0], 0, rows[1], 0], G.dev())
     n = int(b["off"][-1])
     b["q"] = torch.cat([b["q"], torch.full((37, 32, 128), float("nan"), dtype=torch.bfloat16, device=G.dev())])
     table = torch.zeros(4, 1024, dtype=torch.int32, device=G.dev())
     table[:, :b["table"].shape[1]] = b["table"]
     b["table"] = table
     out = torch.full_like(b["q"], 7.0)
-    o = _check(b, CAUSAL, out=out, max_ctx=9000, max_chunk=5000)
+    o = _check(b, CAUSAL, out=out, max_ctx=9000, max_chunk=max_chunk)
     assert o is out and bool((out[n:] == 7.0).all())
 
 
