@@ -60,6 +60,14 @@ def test_short_chunks(B):
     _check(R.chunk_batch(11, 32, 8, 128, 32, [700, 0, 2500], B, G.dev()), CAUSAL)
 
 
+def test_64_rows_over_many_keys():
+    """Enough keys for the chunk kernel to take blocks that the block kernels could: the same rows beside fewer keys go to
+    those, and both agree with the plain form."""
+    b = R.chunk_batch(12, 16, 4, 128, 64, [13000, 12000, 9000, 20, 16000], [64, 1, 33, 64, 0], G.dev())
+    _check(b, CAUSAL, max_ctx=16000)
+    _check(R.chunk_batch(13, 16, 4, 128, 64, [600, 20, 0], [64, 1, 33], G.dev()), CAUSAL)
+
+
 def test_many_sequences():
     """More than 64 sequences: the lookup of a workgroup's share crosses rounds, with empty ones at its edge."""
     rng = np.random.default_rng(5)
