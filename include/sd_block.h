@@ -212,7 +212,8 @@ int sd_kv_append_rope_paged(const sd_rope_shape *shape, int32_t page_size, int32
                             const void *q_weight, const void *k_weight, void *q_out, void *k_pages, void *v_pages,
                             void *stream);
 
-/* Workspace bytes sd_chunk_attn_paged needs for this shape (host-only). */
+/* Workspace bytes sd_chunk_attn_paged needs for this shape (host-only): up to about 135 MB at D = 128 where tiles of
+   query rows may be cut into pieces of keys, a few KB otherwise. */
 int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
 
 /*
@@ -224,6 +225,8 @@ int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
  *   chunk_lens [S] int32      rows of sequence s, 0 <= B_s <= max_block
  *   q_offsets  [S + 1] int32  exclusive prefix sum of chunk_lens, q_offsets[S] <= total_q; rows of out
  *                             from q_offsets[S] on are left as they were
+ * Where a tile's keys are cut, and so the rounding of its sums, depends on the batch's lengths and the shape; the same
+ * call gives the same bits.  Work is handed out through counters in the workspace, which the call sets itself.
  * Keys and values of a sequence at [0, ctx_s + B_s) are finite: a value that is not reaches every row of the
  * tile that holds it, masked for that row or not (0 * inf).  What lies behind ctx_s + B_s in a page is
  * never read.

@@ -7,10 +7,14 @@
 // Pair i is dims (i, R/2 + i), or neighbours (2i, 2i + 1); dims from R on pass.
 //
 // Bound by memory: every element is read once and written once, with about 10 operations between.
+// 8192 bf16 tokens of 32 + 8 heads of 128 (168 MB) take 32.8 us, 5.1 TB/s, the rate of a large copy; prompt
+// chunks of 5.9 thousand tokens appended to pages of 16 (145 MB) 30.9 us, 4.7 TB/s.  One token: 3.2 us, all latency.
 // A lane takes the 8 pairs 8j .. 8j + 7 of one head (two 16-byte vectors in bf16, so both dims of a
 // pair are in one lane and nothing is exchanged), D/16 lanes a head, so a wavefront takes 8 (D = 128) or
 // 16 (D = 64) heads of one token; queries, keys and values of a token are one list of heads.  Each
-// lane computes one angle, and the wavefront hands the cosines and sines round through LDS.
+// lane computes one angle, and the wavefront hands the cosines and sines round through LDS.  Four tokens of
+// the same heads to a workgroup, in place of four parts of one token, were slower (appended chunks 36.2
+// against 34.4 us).
 // Everything between the load and the store is fp32, with one rounding to the element type at the
 // end.  The angle is reduced in 64 bits, in turns (t * w_i / 2 pi less its nearest integer): in
 // 32 bits position 2^20 alone would lose 0.06 rad.
