@@ -605,9 +605,11 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  Without a
     workspace a buffer of the stream's is used; a captured call needs its own."""
     key = ("chunk", _meta(q), _meta(k_pages), _meta(v_pages), _meta(block_table), _meta(ctx_lens), _meta(chunk_lens),
-           _meta(q_offsets), int(max_ctx), int(max_chunk), float(scale), _meta(out))
+           _meta(q_offsets), int(max_ctx), int(max_chunk), float(scale), _meta(out), _meta(workspace))
     c = _call_cache.get(key)
     if c is None:
+        if workspace is not None:
+            _need(workspace, "workspace", None, k_pages.device if isinstance(k_pages, torch.Tensor) else None)
         sh = _chunk_shape(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, max_ctx, max_chunk, scale, out)
         c = _cached_call(key, lambda: sh, chunk_attn_workspace_size)
     _, ref, nbytes = c

@@ -183,3 +183,21 @@ def test_binding_takes_meta_tensors_to_the_device_check():
                                i(4), m(64, dt=torch.float32))
     with pytest.raises(ValueError, match="device tensor"):
         L.chunk_attn_paged(m(5, 4, 128), m(9, 2, 16, 128), m(9, 2, 16, 128), i(3, 4), i(3), i(3), i(4), 0, max_ctx=0, max_chunk=5)
+
+
+def test_chunk_attn_refuses_a_workspace_the_card_cannot_use(monkeypatch):
+    """A workspace in host memory, or one with gaps, is refused before the library is called."""
+    class OnDevice(torch.Tensor):
+        is_cuda = True
+
+    def dev(*s, dt=torch.bfloat16):
+        return torch.zeros(*s, dtype=dt).as_subclass(OnDevice)
+
+    monkeypatch.setattr(L, "lib", lambda: pytest.fail("the library was called"))
+    i32 = torch.int32
+    args = (dev(5, 4, 128), dev(9, 2, 16, 128), dev(9, 2, 16, 128), dev(3, 4, dt=i32), dev(3, dt=i32), dev(3, dt=i32),
+            dev(4, dt=i32), 0)
+    for ws, what in ((torch.zeros(1 << 16, dtype=torch.uint8), "workspace must be a device tensor"),
+                     (dev(1 << 12, 16, dt=torch.uint8)[:, ::2], "workspace must be contiguous"), (7, "workspace must be a torch")):
+        with pytest.raises((ValueError, TypeError), match=what):
+            L.chunk_attn_paged(*args, max_ctx=0, max_chunk=5, workspace=ws)
