@@ -247,13 +247,15 @@ class StreamWorkspace:
         self._bufs = {}
 
     def get(self, nbytes: int, device: torch.device, stream) -> torch.Tensor:
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.get(nbytes, device, None)
         if torch.cuda.is_current_stream_capturing():
             raise ValueError("give a workspace in a call that is captured: the graph keeps its address")
-        key = (device.index, _stream(stream))
+        key = (device.index, _stream(None))
         buf = self._bufs.get(key)
         if buf is None or buf.numel() < nbytes:
-            with torch.cuda.stream(stream):  # None: the current one
-                buf = self._bufs[key] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+            buf = self._bufs[key] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
         return buf
 
 
@@ -471,11 +473,22 @@ def _meta(t):
     return t.shape, t.stride(), t.dtype, t.get_device()
 
 
-def _on_current(t: torch.Tensor) -> None:
+def _on_current(t: torch.Tensor, stream) -> None:
     """The library launches on the current device."""
     cur = _cur_device() if _cur_device is not None else torch.cuda.current_device()
     if t.get_device() != cur:
         raise ValueError(f"the tensors are on {t.device}, the current device is cuda:{cur}")
+    if stream is not None and stream.device_index != cur:
+        raise ValueError(f"the stream is one of cuda:{stream.device_index}, the current device is cuda:{cur}")
+
+
+def _new_like(x: torch.Tensor, stream) -> torch.Tensor:
+    """Packed rows like x's.  They belong to the call's stream: memory that another stream's pending work may still
+    use is not handed to it."""
+    if stream is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _rope_pair(sh: SdRopeShape, x: Optional[torch.Tensor], w, out, which: str, dt, dev, N: int, D: int) -> None:
@@ -527,11 +540,11 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     if c is None:
         sh = _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, rot_scale, q_out, k_out)
         c = _cached_call(key, lambda: sh, lambda _: 0)
-    _on_current(positions)
+    _on_current(positions, stream)
     if q_out is None and q is not None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _new_like(q, stream)
     if k_out is None and k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = _new_like(k, stream)
     _check(lib().sd_qk_norm_rope(c[1], _ptr(q), _ptr(k), positions.data_ptr(), _ptr(inv_freq), _ptr(q_weight),
                                  _ptr(k_weight), _ptr(q_out), _ptr(k_out), _stream(stream)))
     return q_out, k_out
@@ -580,9 +593,9 @@ def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: 
         sh = _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight,
                            k_weight, eps, interleaved, rot_scale, q_out)
         c = _cached_call(key, lambda: sh, lambda _: 0)
-    _on_current(k_pages)
+    _on_current(k_pages, stream)
     if q_out is None and q is not None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = _new_like(q, stream)
     num_pages, _, page_size, _ = k_pages.shape
     _check(lib().sd_kv_append_rope_paged(c[1], page_size, num_pages, block_table.shape[1], block_table.data_ptr(), _ptr(q),
                                          k_new.data_ptr(), v_new.data_ptr(), ctx_lens.data_ptr(), q_offsets.data_ptr(),
@@ -613,9 +626,9 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
         sh = _chunk_shape(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, max_ctx, max_chunk, scale, out)
         c = _cached_call(key, lambda: sh, chunk_attn_workspace_size)
     _, ref, nbytes = c
-    _on_current(q)
+    _on_current(q, stream)
     if out is None:
-        out = torch.empty_like(q)
+        out = _new_like(q, stream)
     if workspace is None:
         workspace = _stream_ws.get(nbytes, q.device, stream)
     num_pages, _, page_size, _ = k_pages.shape

@@ -210,6 +210,19 @@ def test_capture_needs_a_workspace():
             sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], ctx, B, off, CAUSAL, max_ctx=10, max_chunk=80, out=out)
 
 
+def test_a_captured_stream_that_is_not_the_current_one_needs_a_workspace():
+    b = R.chunk_batch(94, 16, 8, 128, 16, [10], [80], G.dev())
+    lens = [_i32(b[x]) for x in ("ctx", "B", "off")]
+    out, x, other = torch.empty_like(b["q"]), torch.zeros(1, device=G.dev()), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        x.add_(1)
+        captured = torch.cuda.current_stream()
+        with torch.cuda.stream(other), pytest.raises(ValueError, match="workspace"):
+            sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], *lens, CAUSAL, max_ctx=10, max_chunk=80, out=out,
+                                stream=captured)
+
+
 def test_two_streams_at_once_without_workspaces():
     """Calls on two streams that run at the same time, growing their buffers: each as alone."""
     batches = [R.chunk_batch(101 + i, 32, 8, 128, 64, [2000 + 900 * i, 0, 64], [150 + 70 * i, 200, 1], G.dev()) for i in range(4)]

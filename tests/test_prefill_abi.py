@@ -1,6 +1,8 @@
 """What the calls that put a prompt into a paged cache refuse, on the host before any device access: the C
 entry points by status code, the binding by exception."""
+import contextlib
 import ctypes
+import types
 
 import pytest
 import torch
@@ -201,3 +203,50 @@ def test_chunk_attn_refuses_a_workspace_the_card_cannot_use(monkeypatch):
                      (dev(1 << 12, 16, dt=torch.uint8)[:, ::2], "workspace must be contiguous"), (7, "workspace must be a torch")):
         with pytest.raises((ValueError, TypeError), match=what):
             L.chunk_attn_paged(*args, max_ctx=0, max_chunk=5, workspace=ws)
+
+
+def test_new_outputs_belong_to_the_call_s_stream(monkeypatch):
+    """Where a stream is given, the outputs that a call makes are allocated on it; a stream of another device is refused."""
+    on, current = [], [None]
+
+    @contextlib.contextmanager
+    def enter(stream):
+        current.append(stream)
+        yield
+        current.pop()
+
+    class OnDevice(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return 0
+
+        @classmethod
+        def __torch_function__(cls, func, types, args=(), kwargs=None):
+            with torch._C.DisableTorchFunctionSubclass():
+                return func(*args, **(kwargs or {}))
+
+    def dev(*s, dt=torch.bfloat16):
+        return torch.zeros(*s, dtype=dt).as_subclass(OnDevice)
+
+    empty, empty_like = torch.empty, torch.empty_like
+    calls = types.SimpleNamespace(**{f: lambda *a: 0 for f in ("sd_qk_norm_rope", "sd_kv_append_rope_paged", "sd_chunk_attn_paged")},
+                                  sd_chunk_attn_workspace_size=L.lib().sd_chunk_attn_workspace_size)
+    monkeypatch.setattr(L, "lib", lambda: calls)
+    monkeypatch.setattr(L, "_cur_device", lambda: 0)
+    monkeypatch.setattr(L, "_call_cache", {})
+    monkeypatch.setattr(torch.cuda, "stream", enter)
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: on.append(current[-1]) or empty(*a, **k))
+    monkeypatch.setattr(torch, "empty_like", lambda *a, **k: on.append(current[-1]) or empty_like(*a, **k))
+    i32, s = torch.int32, types.SimpleNamespace(cuda_stream=5, device_index=0)
+    q, k, pool, table, lens, off = dev(5, 4, 128), dev(5, 2, 128), dev(9, 2, 16, 128), dev(3, 4, dt=i32), dev(3, dt=i32), dev(4, dt=i32)
+    f, pos, ws = dev(64, dt=torch.float32), dev(5, dt=i32), dev(1 << 20, dt=torch.uint8)
+    run = (lambda st: L.qk_norm_rope(q, k, pos, f, stream=st),
+           lambda st: L.kv_append_rope_paged(q, k, k, pool, pool, table, lens, off, f, stream=st),
+           lambda st: L.chunk_attn_paged(q, pool, pool, table, lens, lens, off, 0, max_ctx=0, max_chunk=5, workspace=ws, stream=st))
+    for call, outputs in zip(run, (2, 1, 1)):
+        on.clear()
+        call(s)
+        assert on == [s] * outputs
+        with pytest.raises(ValueError, match="stream is one of cuda:1"):
+            call(types.SimpleNamespace(cuda_stream=6, device_index=1))
