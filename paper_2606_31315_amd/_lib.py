@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 from typing import Optional, Tuple
 
 import torch
@@ -239,9 +240,10 @@ class Workspace:
 _default_ws = Workspace()
 
 
-class StreamWorkspace:
-    """A device scratch buffer per stream, grown on demand: calls on one stream are ordered, and a buffer
-    that is grown out of goes back to the allocator behind its own stream's work."""
+class StreamWorkspace(threading.local):
+    """A device scratch buffer per stream and host thread, grown on demand: a thread's calls on one stream are
+    ordered (the launches of two threads' calls may mix), and a buffer that is grown out of goes back to the allocator
+    behind its own stream's work."""
 
     def __init__(self):
         self._bufs = {}
@@ -616,7 +618,7 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
     without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  Without a
-    workspace a buffer of the stream's is used; a captured call needs its own."""
+    workspace a buffer of the stream's and the host thread's is used; a captured call needs its own."""
     key = ("chunk", _meta(q), _meta(k_pages), _meta(v_pages), _meta(block_table), _meta(ctx_lens), _meta(chunk_lens),
            _meta(q_offsets), int(max_ctx), int(max_chunk), float(scale), _meta(out), _meta(workspace))
     c = _call_cache.get(key)

@@ -1,5 +1,7 @@
 """sd_chunk_attn_paged against the plain form in 64 bits: ragged chunks from no row to hundreds, head
 groups, head sizes, pages that end inside a tile, both masks; what must not change does not."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -237,6 +239,29 @@ def test_two_streams_at_once_without_workspaces():
                             max_chunk=int(b["B"].max()), out=o, stream=streams[i % 2])
     torch.cuda.synchronize()
     assert all(torch.equal(o, r) for o, r in zip(outs, refs))
+
+
+def test_two_threads_on_one_stream_without_workspaces():
+    batches = [R.chunk_batch(111 + i, 32, 8, 128, 64, [2500 + 900 * i, 0], [150 + 70 * i, 200], G.dev()) for i in range(2)]
+    refs = [_run(b, CAUSAL) for b in batches]
+    lens = [[_i32(b[x]) for x in ("ctx", "B", "off")] for b in batches]
+    torch.cuda.synchronize()
+    G.log("sd_chunk_attn_paged from two threads on one stream")
+    outs = [[], []]
+
+    def work(i):
+        b = batches[i]
+        for _ in range(20):
+            outs[i].append(sd.chunk_attn_paged(b["q"], b["kp"], b["vp"], b["table"], *lens[i], CAUSAL,
+                                               max_ctx=int(b["ctx"].max()), max_chunk=int(b["B"].max())))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, refs[i]) for i in range(2) for o in outs[i]) and [len(o) for o in outs] == [20, 20]
 
 
 @pytest.mark.parametrize("S", [1025, 1500], ids=["just_past", "well_past"])

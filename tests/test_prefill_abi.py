@@ -2,6 +2,7 @@
 entry points by status code, the binding by exception."""
 import contextlib
 import ctypes
+import threading
 import types
 
 import pytest
@@ -250,3 +251,26 @@ def test_new_outputs_belong_to_the_call_s_stream(monkeypatch):
         assert on == [s] * outputs
         with pytest.raises(ValueError, match="stream is one of cuda:1"):
             call(types.SimpleNamespace(cuda_stream=6, device_index=1))
+
+
+def test_host_threads_share_no_workspace(monkeypatch):
+    """Two threads' calls on one stream are several launches each, and may mix: each thread has its own buffer."""
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: empty(*a, **k))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(L, "_stream", lambda stream: 5)
+    ws, dev, got = L.StreamWorkspace(), torch.device("cuda", 0), {}
+    go = threading.Barrier(2)  # both alive, so that no buffer is one that the other gave back
+
+    def work(i):
+        go.wait()
+        got[i] = ws.get(1000, dev, None), ws.get(900, dev, None)
+        go.wait()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert got[0][0] is got[0][1] and got[1][0] is got[1][1]
+    assert got[0][0].data_ptr() != got[1][0].data_ptr()
