@@ -263,8 +263,11 @@ def test_host_threads_share_no_workspace(monkeypatch):
     go = threading.Barrier(2)  # both alive, so that no buffer is one that the other gave back
 
     def work(i):
-        go.wait()
+        if i == 1:
+            go.wait()
         got[i] = ws.get(1000, dev, None), ws.get(900, dev, None)
+        if i == 0:
+            go.wait()
         go.wait()
 
     threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
