@@ -219,7 +219,7 @@ int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
 /*
  * sd_block_attn_paged for any number of new rows per sequence: shape->max_block bounds chunk_lens.
  * max_ctx and max_block lie in [0, max_kv_len] and [1, max_kv_len], and ctx_s + B_s <= max_kv_len for
- * every s (their bounds' sum may be more); Hq/Hkv <= 256.
+ * every s (their bounds' sum may be more), which is at most 2^31 - 513; Hq/Hkv <= 256.
  * Everything else is as there: bf16 page pools that already hold the chunk's keys and values, the masks,
  * fp32 softmax and sums with weights rounded to bf16, asynchronous, no synchronisation.
  *   chunk_lens [S] int32      rows of sequence s, 0 <= B_s <= max_block

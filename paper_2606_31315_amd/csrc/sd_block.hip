@@ -710,14 +710,16 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   const long long tiles = ((long long)sh->total_q / P + sh->num_seqs) * sh->num_kv_heads;
   const double units = (double)tiles * sdb::chunk_weight(sdb::kChunkRows) * ((double)L + sdb::kChunkPieceCost);
   if (units >= 4503599627370496.0 || tiles > (1 << 30)) return fail(SD_ERR_INVALID_ARG, "problem too large");
-  // Pieces: a tile of the longest ctx_s + B_s has no more than this many.
+  // The kernels look up to five steps past a key index of 32 bits.
   const long long longest = std::min<long long>(L, (long long)sh->max_ctx + sh->max_block);
+  if (longest > INT32_MAX - 8 * sdb::kChunkKT) return fail(SD_ERR_INVALID_ARG, "max_ctx + max_block too large");
   // Few rows go to the block attention's kernels, whose key tiles keep more wavefronts busy there; from 129 packed
   // rows on only while there are few keys, as those kernels then are bound by their matrix products (us per call,
   // block and chunk kernels, group size 4: 64 rows of 32 sequences at 8192 keys 392 and 324, of 4 at 32768 205 and 162, of 8
   // at 4096 69 and 63, of one at 4096 31 and 41, of 32 at 512 37 and 45; 32 rows of 8 at 4096 44 and 47; single rows of
   // 32 at 8192 173 and 212).
   p->block = sh->max_block <= 64 && G * sh->max_block <= 256 && (G * sh->max_block <= 128 || groups * longest < 200000);
+  // Pieces: a tile of the longest ctx_s + B_s has no more than this many.
   const long long most = (longest + sdb::kChunkPieceCost + sdb::kChunkMinPiece - 1) / sdb::kChunkMinPiece;
   p->slots = most > 1 ? (int)std::min<long long>(sdb::kChunkSlots, tiles * std::min<long long>(most, 64)) : 0;
   p->grid = (int)std::max<long long>(1, std::min<long long>(sdb::kChunkGrid, tiles + p->slots));

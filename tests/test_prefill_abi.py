@@ -134,6 +134,16 @@ def test_chunk_errors():
     assert chunk(chunk_shape(total_q=0), q=None) == L.SD_OK
 
 
+def test_lengths_near_the_end_of_32_bits():
+    """The kernels' key index looks some steps ahead of the last key."""
+    top = 2 ** 31 - 16
+    for block in (1, 5000):
+        for ctx, code in ((top - block, L.SD_ERR_INVALID_ARG), (2 ** 31 - 512 - block, L.SD_ERR_INVALID_ARG),
+                          (2 ** 31 - 513 - block, L.SD_OK)):
+            sh = chunk_shape(num_seqs=1, total_q=1, max_kv_len=top, max_ctx=ctx, max_block=block)
+            assert chunk_ws(sh)[0] == code, (block, ctx)
+
+
 def _t(*shape, dt=torch.bfloat16):
     return torch.zeros(*shape, dtype=dt)
 
