@@ -53,8 +53,9 @@ constexpr int kChunkSpread = 64;      // else a tile is cut where less than this
 constexpr int kChunkEndPieces = 3;    // into this many pieces
 constexpr int kChunkPieceExtra = 512; // keys' worth of cutting: sums filed and joined
 
-// Relative time of a key by the tile's rows: wavefronts without rows leave theirs to the others.
-SDB_HD int chunk_weight(int rows) { return plan_max((rows + 31) / 32, 3); }
+// Relative time of a key by the tile's rows (a step of 256 rows takes 3390 cycles, of 128 2720, of 64 2590).  Those
+// of sequences of few rows are bound by memory, and by less of it the more of them run at once.
+SDB_HD int chunk_weight(int rows, bool few = false) { return plan_max((rows + 31) / 32, few ? 3 : 5); }
 
 struct ChunkSeq {
   int ctx, B, P, G, causal;
@@ -62,7 +63,7 @@ struct ChunkSeq {
   SDB_HD int rows(int j) const { return plan_min(P, B - P * j) * G; }           // of tile j
   SDB_HD int keys(int j) const { return ctx + (causal ? plan_min(P * (j + 1), B) : B); }
   // Work of tile j, and of the tiles before it (which are all full): whole numbers, below 2^53 (the host checks).
-  SDB_HD double units(int j) const { return (double)chunk_weight(rows(j)) * ((double)keys(j) + kChunkPieceCost); }
+  SDB_HD double units(int j) const { return (double)chunk_weight(rows(j), few()) * ((double)keys(j) + kChunkPieceCost); }
   SDB_HD double before(int j) const {
     const double n = j, each = (double)(causal ? ctx : ctx + B) + kChunkPieceCost;
     return chunk_weight(P * G) * (n * each + (causal ? n * (n + 1) / 2 * P : 0));

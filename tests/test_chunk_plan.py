@@ -51,5 +51,12 @@ def test_no_item_is_long(plan, S, Hkv, G, ctx, B):
     assert largest < 1.6 or largest * units < 2 * share
 
 
+@pytest.mark.parametrize("S,ctx,B", [(1, 4000, 400), (2, 1800, 200), (2, 4000, 200)])
+def test_the_last_tiles_of_small_batches_are_cut_too(plan, S, ctx, B):
+    """A tile of 64 rows takes three quarters of a full one's time."""
+    items, pieces, _ = _run(plan, 8, 4, 1, [ctx] * S, [B] * S)
+    assert items == pieces > 0
+
+
 def test_empty(plan):
     assert _run(plan, 8, 4, 1, [5, 0], [0, 0]) == (0, 0, 0.0)
