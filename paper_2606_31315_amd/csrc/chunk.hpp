@@ -406,8 +406,15 @@ __device__ __forceinline__ void chunk_phase_end() {
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-template <int D, bool PLANNED>
+// How the workgroups find their work: items of the plan; whole tiles by their index; the same with tiles of 128
+// rows, whose steps the two halves of the workgroup take in turn and join at the end: twice the workgroups, each
+// with half the steps of half the rows, where a batch leaves CUs idle (100 rows at 500 keys, 32 heads on 8: 17.2 us, of
+// which ten steps of 256 rows would take 21.8; a step of 128 keys takes the 3400 cycles of one of 64 with 256 rows).
+enum ChunkMode { kPlanned, kDirect, kHalves };
+
+template <int D, ChunkMode MODE>
 __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
+  constexpr bool PLANNED = MODE == kPlanned, HALVES = MODE == kHalves;
   using T = ChunkTile<D>;
   constexpr int NST = D / 16, NDT = D / 32, EB = 2;
   __shared__ __attribute__((aligned(1024))) char stages[4 * T::STAGEB];  // a K and a V tile each
@@ -465,15 +472,16 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
 
     // ---- query operands: element e of step st is dim st*16 + h*8 + e of row m ----
     bf16x8 qop[NST];
-    const int m = wave * 32 + l32, mc = min(m, M - 1), mp = mc / a.G;  // rows past the tile: its last
+    const int rwave = HALVES ? wave & 3 : wave;  // which 32 rows
+    const int m = rwave * 32 + l32, mc = min(m, M - 1), mp = mc / a.G;  // rows past the tile: its last
     const int lim = a.causal ? e.ctx + p0 + mp + 1 : n;            // keys the row sees
     {
       const char *qrow = (const char *)a.q + ((size_t)(e.qoff + p0 + mp) * a.Hq + g * a.G + (mc - mp * a.G)) * D * EB;
 #pragma unroll
       for (int st = 0; st < NST; ++st) qop[st] = *(const bf16x8 *)(qrow + (st * 16 + h * 8) * EB);
     }
-    const int vis_all = min(k1, a.causal ? e.ctx + p0 + min(wave * 32, M - 1) / a.G + 1 : n);  // keys that all its rows see
-    const bool act = wave * 32 < M;  // the wavefront has rows
+    const int vis_all = min(k1, a.causal ? e.ctx + p0 + min(rwave * 32, M - 1) / a.G + 1 : n);  // keys that all its rows see
+    const bool act = rwave * 32 < M;  // the wavefront has rows
 
     f32x16 oacc[NDT];
     float m_run = -INFINITY, l_run = 0.f;
@@ -520,7 +528,9 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
     const unsigned vaddr = lds0 + T::TILEB + vrow * T::ROWB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ T::swz_v(vrow)) << 4) +
                            ((lane & 1) << 3);
 
-    const int nsteps = (k1 - k0 + kChunkKT - 1) / kChunkKT;
+    // Step t of a wavefront takes tile t; of a half's, tile 2t or 2t + 1, which may lie behind the last key.
+    const int nsteps = (k1 - k0 + kChunkKT * (HALVES ? 2 : 1) - 1) / (kChunkKT * (HALVES ? 2 : 1));
+    auto tile_of = [&](int t) __attribute__((always_inline)) { return HALVES ? 2 * t + (wave >= 4) : t; };
     // ---- the products and the softmax of a step ----
     f32x16 sacc[2];  // [kb]: register i is key kb*32 + 8*(i/4) + 4h + i%4 of row l32
     bf16x8 pop[4];   // the weights of 16 keys each
@@ -529,7 +539,7 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
     constexpr int NP = 4 * NDT, NPQ = NP + 2 * NST, kAhead = 6;
     auto products = [&](auto from_c, auto to_c, int t, auto loads_c) __attribute__((always_inline)) {
       constexpr int FROM = decltype(from_c)::value, TO = decltype(to_c)::value;
-      unsigned va = vaddr + ((t - 1) & 3) * T::STAGEB, ka = kaddr + (t & 3) * T::STAGEB;
+      unsigned va = vaddr + (tile_of(t - 1) & 3) * T::STAGEB, ka = kaddr + (tile_of(t) & 3) * T::STAGEB;
       asm("" : "+v"(va), "+v"(ka));  // the operands' addresses are made here, in the products' shadow, not kept in registers
       bf16x8 op[NPQ];
       auto read = [&](int i) __attribute__((always_inline)) {
@@ -629,46 +639,94 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
 #pragma unroll
       for (int i = 0; i < T::NV; ++i) load(i);
     };
-    {
-      const int id0 = page_of(0), id1 = page_of(1);
-      start(0, id0);
-      load_all();
-      start(1, id1);
-      load_all();
-    }
-    int id = page_of(2);
+    if constexpr (HALVES) {
+      // Both tiles of a step are fetched together, and the ring holds two steps: the first half fetches K of step t + 1
+      // in phase 2t, as its stages were last read in phase 2t - 1, to be there for phase 2t + 2; the second half V of
+      // step t + 1 in phase 2t + 2, as its stages were last read in phase 2t + 1, for phase 2t + 4.  (Each half its own
+      // tiles, three phases ahead, was no faster.)
+      auto fetch = [&](int t, int i0, int i1) __attribute__((always_inline)) {
+        start(2 * t, i0);
+        load_all();
+        start(2 * t + 1, i1);
+        load_all();
+      };
+      {
+        const int i0 = page_of(0), i1 = page_of(1), i2 = page_of(2), i3 = page_of(3);
+        fetch(0, i0, i1);
+        fetch(1, i2, i3);
+      }
+      int i0 = page_of(4), i1 = page_of(5);
 #pragma unroll
-    for (int st = 0; st < NST; ++st) asm volatile("" : "+v"(qop[st]));  // waited for here, not in the loop
-    chunk_phase_end<T::NV>();                // tile 0 is here
-    if (second) chunk_phase_end<-1>();  // phase 0
-    start(2, id);
-    id = page_of(3);
-    load_all();
-    if (act) products(Int<NP>{}, Int<NPQ>{}, 0, Int<0>{});
-    auto between = [&]() __attribute__((always_inline)) {  // the products of a step and its softmax
-      if (second) chunk_phase_end<T::NV>();  // the next tile is here
+      for (int st = 0; st < NST; ++st) asm volatile("" : "+v"(qop[st]));
+      chunk_phase_end<2 * T::NV>();       // the first step's tiles are here
+      if (second) chunk_phase_end<-1>();  // phase 0
+      if (act) products(Int<NP>{}, Int<NPQ>{}, 0, Int<0>{});
+      if (second) chunk_phase_end<0>();
       else chunk_phase_end<-1>();
-    };
-    auto behind = [&]() __attribute__((always_inline)) {  // the softmax
+      if (act) softmax(k0 + tile_of(0) * kChunkKT);
       if (second) chunk_phase_end<-1>();
-      else chunk_phase_end<T::NV>();
-    };
-    between();
-    if (act) softmax(k0);
-    behind();
-    for (int t = 1; t < nsteps; ++t) {
-      start(t + 2, id);
-      id = page_of(t + 3);
-      if (act) {
-        __builtin_amdgcn_s_setprio(1);
-        products(Int<0>{}, Int<NPQ>{}, t, Int<1>{});
-        __builtin_amdgcn_s_setprio(0);
-      } else {
+      else chunk_phase_end<0>();
+      for (int t = 1; t < nsteps; ++t) {
+        if (!second) fetch(t + 1, i0, i1);
+        if (act) {
+          __builtin_amdgcn_s_setprio(1);
+          products(Int<0>{}, Int<NPQ>{}, t, Int<0>{});
+          __builtin_amdgcn_s_setprio(0);
+        }
+        if (second) {
+          chunk_phase_end<0>();
+          fetch(t + 1, i0, i1);
+        } else {
+          chunk_phase_end<-1>();
+        }
+        i0 = page_of(2 * t + 4);
+        i1 = page_of(2 * t + 5);
+        if (act) softmax(k0 + tile_of(t) * kChunkKT);
+        if (second) chunk_phase_end<-1>();
+        else chunk_phase_end<0>();
+      }
+    } else {
+      {
+        const int id0 = page_of(0), id1 = page_of(1);
+        start(0, id0);
+        load_all();
+        start(1, id1);
         load_all();
       }
+      int id = page_of(2);
+#pragma unroll
+      for (int st = 0; st < NST; ++st) asm volatile("" : "+v"(qop[st]));  // waited for here, not in the loop
+      chunk_phase_end<T::NV>();                // tile 0 is here
+      if (second) chunk_phase_end<-1>();  // phase 0
+      start(2, id);
+      id = page_of(3);
+      load_all();
+      if (act) products(Int<NP>{}, Int<NPQ>{}, 0, Int<0>{});
+      auto between = [&]() __attribute__((always_inline)) {  // the products of a step and its softmax
+        if (second) chunk_phase_end<T::NV>();  // the next tile is here
+        else chunk_phase_end<-1>();
+      };
+      auto behind = [&]() __attribute__((always_inline)) {  // the softmax
+        if (second) chunk_phase_end<-1>();
+        else chunk_phase_end<T::NV>();
+      };
       between();
-      if (act) softmax(k0 + t * kChunkKT);
+      if (act) softmax(k0);
       behind();
+      for (int t = 1; t < nsteps; ++t) {
+        start(t + 2, id);
+        id = page_of(t + 3);
+        if (act) {
+          __builtin_amdgcn_s_setprio(1);
+          products(Int<0>{}, Int<NPQ>{}, t, Int<1>{});
+          __builtin_amdgcn_s_setprio(0);
+        } else {
+          load_all();
+        }
+        between();
+        if (act) softmax(k0 + t * kChunkKT);
+        behind();
+      }
     }
     if constexpr (PLANNED) {
       if (tid == 0) ahead = chunk_take(a, queue);
@@ -680,7 +738,47 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
     // ---- output: register i of oacc[dt] is dim dt*32 + 8*(i/4) + 4h + i%4 of row l32 ----
     const float2 pl = pair_x32(l_run);
     const float lsum = pl.x + pl.y;
-    if (m < M && piece < 0) {
+    if constexpr (HALVES) {
+      // Each half takes the dims of half of O and gives its partner's to it.
+      float4 *const give = (float4 *)stages + wave * (NDT * 2) * 64 + lane, *const take = (float4 *)stages + (wave ^ 4) * (NDT * 2) * 64 + lane;
+      float2 *const ml = (float2 *)(stages + 8 * (NDT * 2) * 64 * 16);
+      auto give_half = [&](auto own_c) __attribute__((always_inline)) {
+        constexpr int OTHER = decltype(own_c)::value ? 0 : NDT / 2;
+#pragma unroll
+        for (int d = 0; d < NDT / 2; ++d)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const f32x16 &o = oacc[OTHER + d];
+            give[(d * 4 + c) * 64] = float4{o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]};
+          }
+      };
+      if (second) give_half(Int<1>{});
+      else give_half(Int<0>{});
+      if (h == 0) ml[wave * 32 + l32] = float2{m_run, lsum};
+      __syncthreads();
+      const float2 x = ml[(wave ^ 4) * 32 + l32];
+      const float mx = fmaxf(m_run, x.x);
+      const float wo = m_run == -INFINITY ? 0.f : fast_exp2(m_run - mx), wx = x.x == -INFINITY ? 0.f : fast_exp2(x.x - mx);
+      const float inv = 1.f / (lsum * wo + x.y * wx);
+      auto join = [&](auto own_c) __attribute__((always_inline)) {
+        constexpr int OWN = decltype(own_c)::value ? NDT / 2 : 0;
+        char *orow = (char *)a.out + ((size_t)(e.qoff + p0 + mp) * a.Hq + g * a.G + (m - mp * a.G)) * D * EB;
+#pragma unroll
+        for (int d = 0; d < NDT / 2; ++d)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const f32x16 &o = oacc[OWN + d];
+            const float4 y = take[(d * 4 + c) * 64];
+            const float z0 = (o[4 * c] * wo + y.x * wx) * inv, z1 = (o[4 * c + 1] * wo + y.y * wx) * inv;
+            const float z2 = (o[4 * c + 2] * wo + y.z * wx) * inv, z3 = (o[4 * c + 3] * wo + y.w * wx) * inv;
+            *(uint2 *)(orow + ((OWN + d) * 32 + c * 8 + h * 4) * EB) = uint2{cvt_pk_bf16(z0, z1), cvt_pk_bf16(z2, z3)};
+          }
+      };
+      if (m < M) {
+        if (second) join(Int<1>{});
+        else join(Int<0>{});
+      }
+    } else if (m < M && piece < 0) {
       const float inv = 1.f / lsum;
       char *orow = (char *)a.out + ((size_t)(e.qoff + p0 + mp) * a.Hq + g * a.G + (m - mp * a.G)) * D * EB;
 #pragma unroll

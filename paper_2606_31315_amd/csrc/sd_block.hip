@@ -687,6 +687,7 @@ struct ChunkPlan {
   bool block;             // small blocks: the block attention's kernels
   sd_attn_shape block_sh; // their shape
   bool direct;            // few short tiles: one launch, a workgroup per tile
+  bool halves;            // of half the rows, whose keys the two halves of a workgroup share
   int slots, grid;        // pieces and workgroups at most
   size_t off_entries, off_prefix, off_merges, off_ml, off_o, total;
 };
@@ -725,10 +726,16 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   p->grid = (int)std::max<long long>(1, std::min<long long>(sdb::kChunkGrid, tiles + p->slots));
   // A plan that cuts tiles into np pieces saves all but one np-th of their steps, and costs two launches more
   // and the pieces' sums, about 16 steps' time (both sides: 100 rows at a context of 500, 26 us planned and
-  // cut in two, 21 us direct).
-  const long long np = std::max<long long>(2, tiles > 0 ? sdb::kChunkGrid / tiles : 2);
-  p->direct = tiles <= sdb::kChunkGrid && (longest + sdb::kChunkKT - 1) / sdb::kChunkKT * (np - 1) <= 16 * np;
-  if (p->direct) p->slots = 0, p->grid = (int)std::max<long long>(1, tiles);
+  // cut in two, 21 us direct).  Tiles of 128 rows whose keys the two halves of a workgroup share take three fifths of
+  // the time of one of 256 rows, where there are CUs for twice as many (100 rows at 500 keys 17 and 22 us, at 1700 33
+  // and, planned, 35, at 2600 with 300 rows 48 and 46; two sequences of 200 rows at 1800 36 and 43, at 4000
+  // 64 and 56; four at 2000 47 and 63, at 8000 135 and 165).
+  const long long steps = (longest + sdb::kChunkKT - 1) / sdb::kChunkKT, np = std::max<long long>(2, tiles > 0 ? sdb::kChunkGrid / tiles : 2);
+  const int P2 = sdb::kChunkRows / 2 / G;
+  const long long half = P2 > 0 ? ((long long)sh->total_q / P2 + sh->num_seqs) * sh->num_kv_heads : sdb::kChunkGrid + 1;
+  p->halves = half <= sdb::kChunkGrid && steps * (3 * np - 5) <= 16 * 5 * np;
+  p->direct = p->halves || (tiles <= sdb::kChunkGrid && steps * (np - 1) <= 16 * np);
+  if (p->direct) p->slots = 0, p->grid = (int)std::max<long long>(1, p->halves ? half : tiles);
   p->off_entries = align256(sizeof(sdb::ChunkHead));
   p->off_prefix = align256(p->off_entries + sizeof(sdb::ChunkEntry) * sh->num_seqs);
   p->off_merges = align256(p->off_prefix + sizeof(int) * sdb::kChunkQueues * ((groups + sdb::kChunkQueues - 1) / sdb::kChunkQueues));
@@ -794,7 +801,7 @@ int sd_chunk_attn_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_
   a.Hq = sh->num_q_heads;
   a.Hkv = sh->num_kv_heads;
   a.G = a.Hq / a.Hkv;
-  a.P = sdb::kChunkRows / a.G;
+  a.P = (p.halves ? sdb::kChunkRows / 2 : sdb::kChunkRows) / a.G;
   a.page_log2 = log2;
   a.max_pages = max_pages;
   a.num_pages = num_pages;
@@ -814,13 +821,15 @@ int sd_chunk_attn_paged(const sd_attn_shape *sh, int32_t page_size, int32_t num_
   const bool wide = sh->head_dim == 128;
   const dim3 grid(p.grid), block(512);
   if (p.direct) {
-    if (wide) hipLaunchKernelGGL((sdb::chunk_attn_kernel<128, false>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((sdb::chunk_attn_kernel<64, false>), grid, block, 0, st, a);
+    if (p.halves && wide) hipLaunchKernelGGL((sdb::chunk_attn_kernel<128, sdb::kHalves>), grid, block, 0, st, a);
+    else if (p.halves) hipLaunchKernelGGL((sdb::chunk_attn_kernel<64, sdb::kHalves>), grid, block, 0, st, a);
+    else if (wide) hipLaunchKernelGGL((sdb::chunk_attn_kernel<128, sdb::kDirect>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((sdb::chunk_attn_kernel<64, sdb::kDirect>), grid, block, 0, st, a);
     return check_launch("sd_chunk_attn_paged");
   }
   hipLaunchKernelGGL(sdb::chunk_plan_kernel, dim3(1), dim3(sdb::kChunkPlanThreads), 0, st, a);
-  if (wide) hipLaunchKernelGGL((sdb::chunk_attn_kernel<128, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((sdb::chunk_attn_kernel<64, true>), grid, block, 0, st, a);
+  if (wide) hipLaunchKernelGGL((sdb::chunk_attn_kernel<128, sdb::kPlanned>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((sdb::chunk_attn_kernel<64, sdb::kPlanned>), grid, block, 0, st, a);
   if (p.slots > 1) {
     const dim3 merge(std::min(p.slots / 2 * sdb::kChunkMergeUnits, 1024)), threads(256);
     if (wide) hipLaunchKernelGGL(sdb::chunk_merge_kernel<128>, merge, threads, 0, st, a);

@@ -56,6 +56,30 @@ def test_parity(name, Hq, Hkv, D, page, ctx, B, mask):
     _check(R.chunk_batch(len(name), Hq, Hkv, D, page, ctx, B, G.dev()), mask)
 
 
+@pytest.mark.parametrize("name,Hq,Hkv,D,page,ctx,B", CASES, ids=[c[0] for c in CASES])
+def test_parity_planned(name, Hq, Hkv, D, page, ctx, B):
+    """The same rows beside a long context without rows, whose bound has the batch planned."""
+    _check(R.chunk_batch(len(name) + 300, Hq, Hkv, D, page, ctx + [10500], B + [0], G.dev()), CAUSAL)
+
+
+@pytest.mark.parametrize("mask", [CAUSAL, BIDIR], ids=["causal", "bidir"])
+@pytest.mark.parametrize("Hq,Hkv,D", [(32, 8, 128), (24, 8, 64)])
+def test_many_short_chunks(Hq, Hkv, D, mask):
+    """More tiles of 128 rows than CUs, fewer of 256: whole tiles in one launch."""
+    B = [65, 1, 90, 0, 130, 64, 65, 66, 2, 33, 100, 127, 5, 70]
+    ctx = [0, 77, 300, 1000, 5, 64, 63, 640, 1, 0, 129, 400, 1000, 31]
+    _check(R.chunk_batch(14, Hq, Hkv, D, 16, ctx, B, G.dev()), mask)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(32, 8, 128), (8, 8, 64), (128, 1, 128), (129, 1, 64)])
+def test_lengths_about_a_step(Hq, Hkv, D):
+    """One tile, two, three and four of 64 keys, or one less or more: a step's second tile may hold one key or none."""
+    for ctx in (0, 1, 54, 55, 56, 63, 64, 118, 119, 120, 183, 190):
+        b = R.chunk_batch(400 + ctx, Hq, Hkv, D, 16, [ctx, 200], [9, 2], G.dev())
+        _check(b, CAUSAL, max_chunk=208)
+        _check(b, BIDIR, max_chunk=208)
+
+
 @pytest.mark.parametrize("B", [[1, 1, 1], [5, 16, 0], [17, 64, 33]], ids=["tokens", "blocks", "to_64_rows"])
 def test_short_chunks(B):
     """Batches that the block attention's kernels take."""
