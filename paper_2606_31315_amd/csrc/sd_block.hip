@@ -705,21 +705,20 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   const int G = sh->num_q_heads / sh->num_kv_heads;
   if (G > sdb::kChunkRows) return fail(SD_ERR_UNSUPPORTED, "group size %d exceeds %d", G, sdb::kChunkRows);
   if (!(sh->scale >= 0.f) || isinf(sh->scale)) return fail(SD_ERR_INVALID_ARG, "scale must be finite and >= 0");
-  // Query tiles at most; the plan counts items in 32 bits and work in doubles.
+  // Query tiles at most, all rows' and each sequence's last or max_block's of each; the plan counts items in 32 bits
+  // and work in doubles.
+  auto tiles_of = [&](int positions) {
+    const long long rows = (long long)sh->total_q / positions + sh->num_seqs, each = (sh->max_block - 1) / positions + 1;
+    return std::min(rows, sh->num_seqs * each) * sh->num_kv_heads;
+  };
   const int P = sdb::kChunkRows / G, L = sh->max_kv_len;
   const long long groups = (long long)sh->num_seqs * sh->num_kv_heads;
-  const long long tiles = ((long long)sh->total_q / P + sh->num_seqs) * sh->num_kv_heads;
+  const long long tiles = tiles_of(P);
   const double units = (double)tiles * sdb::chunk_weight(sdb::kChunkRows) * ((double)L + sdb::kChunkPieceCost);
   if (units >= 4503599627370496.0 || tiles > (1 << 30)) return fail(SD_ERR_INVALID_ARG, "problem too large");
   // The kernels look up to five steps past a key index of 32 bits.
   const long long longest = std::min<long long>(L, (long long)sh->max_ctx + sh->max_block);
   if (longest > INT32_MAX - 8 * sdb::kChunkKT) return fail(SD_ERR_INVALID_ARG, "max_ctx + max_block too large");
-  // Few rows go to the block attention's kernels, whose key tiles keep more wavefronts busy there; from 129 packed
-  // rows on only while there are few keys, as those kernels then are bound by their matrix products (us per call,
-  // block and chunk kernels, group size 4: 64 rows of 32 sequences at 8192 keys 392 and 324, of 4 at 32768 205 and 162, of 8
-  // at 4096 69 and 63, of one at 4096 31 and 41, of 32 at 512 37 and 45; 32 rows of 8 at 4096 44 and 47; single rows of
-  // 32 at 8192 173 and 212).
-  p->block = sh->max_block <= 64 && G * sh->max_block <= 256 && (G * sh->max_block <= 128 || groups * longest < 200000);
   // Pieces: a tile of the longest ctx_s + B_s has no more than this many.
   const long long most = (longest + sdb::kChunkPieceCost + sdb::kChunkMinPiece - 1) / sdb::kChunkMinPiece;
   p->slots = most > 1 ? (int)std::min<long long>(sdb::kChunkSlots, tiles * std::min<long long>(most, 64)) : 0;
@@ -732,8 +731,18 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   // 64 and 56; four at 2000 47 and 63, at 8000 135 and 165).
   const long long steps = (longest + sdb::kChunkKT - 1) / sdb::kChunkKT, np = std::max<long long>(2, tiles > 0 ? sdb::kChunkGrid / tiles : 2);
   const int P2 = sdb::kChunkRows / 2 / G;
-  const long long half = P2 > 0 ? ((long long)sh->total_q / P2 + sh->num_seqs) * sh->num_kv_heads : sdb::kChunkGrid + 1;
+  const long long half = P2 > 0 ? tiles_of(P2) : sdb::kChunkGrid + 1;
   p->halves = half <= sdb::kChunkGrid && steps * (3 * np - 5) <= 16 * 5 * np;
+  // Few rows go to the block attention's kernels, whose key tiles keep more wavefronts busy there; from 129 packed
+  // rows on only while there are few keys, as those kernels then are bound by their matrix products (us per call,
+  // block and chunk kernels, group size 4: 64 rows of 32 sequences at 8192 keys 392 and 324, of 4 at 32768 205 and 162, of
+  // one at 4096 31 and 40, of 32 at 512 35 and 46; 32 rows of 8 at 4096 44 and 47; single rows of 32 at 8192
+  // 173 and 212).  Beside the halves their time is that of a workgroup's rows, more of them at once the more heads there
+  // are (8 kv heads: 48 rows of 16 sequences at 500 keys 32 and 22, of 4 19.5 and 17.1, of one 16.4 and 16.8; at
+  // 1000 keys of 16 41 and 35, of 4 25 and 24, of one 19 and 23; 16 rows of 16 at 500 16.9 and 16.3, of 8 at 1000 16 and 20).
+  const long long packed = (long long)G * sh->max_block;
+  p->block = sh->max_block <= 64 && packed <= 256 && (packed <= 128 || groups * longest < 200000) &&
+             !(p->halves && packed * (64 + groups) >= 10000 + 460 * steps);
   p->direct = p->halves || (tiles <= sdb::kChunkGrid && steps * (np - 1) <= 16 * np);
   if (p->direct) p->slots = 0, p->grid = (int)std::max<long long>(1, p->halves ? half : tiles);
   p->off_entries = align256(sizeof(sdb::ChunkHead));

@@ -86,9 +86,21 @@ def test_short_chunks(B):
     _check(R.chunk_batch(11, 32, 8, 128, 32, [700, 0, 2500], B, G.dev()), CAUSAL)
 
 
+@pytest.mark.parametrize("mask", [CAUSAL, BIDIR], ids=["causal", "bidir"])
+@pytest.mark.parametrize("Hq,Hkv,D,most", [(32, 8, 128, 24), (32, 8, 128, 64), (32, 8, 64, 17), (8, 8, 64, 64)])
+def test_blocks_of_many_sequences(Hq, Hkv, D, most, mask):
+    """Blocks that the block kernels could take beside contexts short enough for the chunk kernel's halves, and the
+    same beside one that is not."""
+    rng = np.random.default_rng(most)
+    B, ctx = rng.integers(0, most + 1, 14), rng.integers(0, 450, 14)
+    B[:3], ctx[:3] = [most, 0, 1], [449, 13, 0]
+    _check(R.chunk_batch(15, Hq, Hkv, D, 16, ctx, B, G.dev()), mask)
+    ctx[4] = 5000
+    _check(R.chunk_batch(16, Hq, Hkv, D, 16, ctx, B, G.dev()), mask)
+
+
 def test_64_rows_over_many_keys():
-    """Enough keys for the chunk kernel to take blocks that the block kernels could: the same rows beside fewer keys go to
-    those, and both agree with the plain form."""
+    """Enough keys for the chunk kernel to take blocks that the block kernels could, and the same rows beside fewer keys."""
     b = R.chunk_batch(12, 16, 4, 128, 64, [13000, 12000, 9000, 20, 16000], [64, 1, 33, 64, 0], G.dev())
     _check(b, CAUSAL, max_ctx=16000)
     _check(R.chunk_batch(13, 16, 4, 128, 64, [600, 20, 0], [64, 1, 33], G.dev()), CAUSAL)
