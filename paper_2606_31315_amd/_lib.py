@@ -468,11 +468,13 @@ def _norm_weight(w: Optional[torch.Tensor], name: str, like: torch.Tensor) -> No
         _need(w, name, like.dtype, like.device)
 
 
-def _meta(t):
-    """All that the checks of a tensor look at: calls of tensors like those of an earlier one need not repeat them."""
-    if not isinstance(t, torch.Tensor):
-        return type(t)
-    return t.shape, t.stride(), t.dtype, t.get_device()
+def _metas(*ts):
+    """All that the checks of tensors look at: calls of tensors like those of an earlier one need not repeat them.
+    (Reading it is most of a call's host time; a call of a function per tensor would be a quarter more.)"""
+    try:
+        return tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.get_device()) for t in ts])
+    except AttributeError:  # something else among them, which the checks will name
+        return tuple([_metas(t) if isinstance(t, torch.Tensor) else type(t) for t in ts])
 
 
 def _on_current(t: torch.Tensor, stream) -> None:
@@ -536,8 +538,8 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     projection); inv_freq [R/2] fp32 rotates the first R dims (None: none).  q or k may be None; an output
     may be its input.  Returns (q_out, k_out)."""
     interleaved = bool(interleaved)
-    key = ("rope", _meta(q), _meta(k), _meta(positions), _meta(inv_freq), _meta(q_weight), _meta(k_weight), eps,
-           interleaved, rot_scale, _meta(q_out), _meta(k_out))
+    key = ("rope", eps, interleaved, rot_scale,
+           _metas(q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out))
     c = _call_cache.get(key)
     if c is None:
         sh = _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, rot_scale, q_out, k_out)
@@ -587,9 +589,8 @@ def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: 
     """qk_norm_rope at positions ctx_s + i, with k and v written into page pools [num_pages, Hkv, page_size, D]
     through block_table [S, max_pages] (sd_kv_append_rope_paged).  q may be None (append only).  Returns q_out."""
     interleaved = bool(interleaved)
-    key = ("append", _meta(q), _meta(k_new), _meta(v_new), _meta(k_pages), _meta(v_pages), _meta(block_table),
-           _meta(ctx_lens), _meta(q_offsets), _meta(inv_freq), _meta(q_weight), _meta(k_weight), eps, interleaved,
-           rot_scale, _meta(q_out))
+    key = ("append", eps, interleaved, rot_scale,
+           _metas(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight, k_weight, q_out))
     c = _call_cache.get(key)
     if c is None:
         sh = _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight,
@@ -619,8 +620,8 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
     without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  Without a
     workspace a buffer of the stream's and the host thread's is used; a captured call needs its own."""
-    key = ("chunk", _meta(q), _meta(k_pages), _meta(v_pages), _meta(block_table), _meta(ctx_lens), _meta(chunk_lens),
-           _meta(q_offsets), int(max_ctx), int(max_chunk), float(scale), _meta(out), _meta(workspace))
+    key = ("chunk", int(max_ctx), int(max_chunk), float(scale),
+           _metas(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, out, workspace))
     c = _call_cache.get(key)
     if c is None:
         if workspace is not None:
