@@ -536,7 +536,7 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
     bf16x8 pop[4];   // the weights of 16 keys each
     // Products FROM .. TO - 1 of a step: NP of O^T += V^T P^T (tile t - 1), then those of S^T = K Q^T (tile t).
     // Each product's left operand is read kAhead products before it; the order stays as written.
-    constexpr int NP = 4 * NDT, NPQ = NP + 2 * NST, kAhead = 8;
+    constexpr int NP = 4 * NDT, NPQ = NP + 2 * NST, kAhead = D == 128 ? 8 : 6;
     auto operand = [&](int i, unsigned va, unsigned ka) __attribute__((always_inline)) {
       if (i < NP) {
         const int ks = i / NDT, dt = i % NDT;
@@ -553,7 +553,9 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
     };
     // The first operands of P V of step t are read at the end of its softmax, before the phase that multiplies, so
     // that its products need not wait for them (2048 rows at 65536 keys 1.91 -> 1.85 ms, 8192 rows 501 -> 489 us).  V of step
-    // t is there by then, but not in a workgroup of halves.
+    // t is there by then, but not in a workgroup of halves.  At head_dim 64 the softmax is the longer phase, and what is
+    // added to it costs more (1.25 ms without, 1.33 with).
+    constexpr bool EARLY = D == 128 && !HALVES;
     bf16x8 first[kAhead];
     auto read_first = [&](int t) __attribute__((always_inline)) {
       unsigned va = vaddr + (tile_of(t) & 3) * T::STAGEB;
@@ -569,7 +571,7 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
       auto read = [&](int i) __attribute__((always_inline)) { op[i] = operand(i, va, ka); };
 #pragma unroll
       for (int i = FROM; i < FROM + kAhead; ++i) {
-        if (FROM == 0 && !HALVES) {
+        if (FROM == 0 && EARLY) {
           op[i] = first[i];
         } else {
           read(i);
@@ -721,7 +723,7 @@ __global__ __launch_bounds__(512) void chunk_attn_kernel(ChunkArgs a) {
         else chunk_phase_end<-1>();
       };
       auto behind = [&](int t) __attribute__((always_inline)) {  // the softmax of step t
-        if (act) read_first(t);
+        if (EARLY && act) read_first(t);
         if (second) chunk_phase_end<-1>();
         else chunk_phase_end<T::NV>();
       };
