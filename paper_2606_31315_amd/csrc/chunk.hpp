@@ -15,14 +15,16 @@
 // to key; sums and O stay fp32.
 //
 // Bound, for long chunks, by the matrix cores and the power they draw: 2048 rows at 65536 keys (32 heads on 4) take
-// 1.87 to 1.96 ms from card to card, 1.14 to 1.19 PFLOP/s, where a matrix product of 16384^3 reaches 1.37.  The matrix
-// units are busy 60% of the cycles at a clock of 1.9 GHz; without the tile loads, in a copy that skips them, 65% at
-// 1.92, without LDS reads 77% at 1.81, without either LDS reads or softmax 80% at 1.94.  LDS reads (256 KB a step
-// for 2048 cycles of products, 128 bytes a cycle) are the next bound, without bank conflicts; the L2 serves 96% of the tile
-// loads.  At head_dim 64, half the products to a softmax: 1.21 to 1.24 ms, 0.90 to 0.93 PFLOP/s.
+// 1.84 to 1.90 ms from card to card, 1.17 to 1.21 PFLOP/s, where a matrix product of 16384^3 reaches 1.37.  The matrix
+// units are busy 62% of the cycles at a clock of 2.0 GHz (a step is 2048 cycles of products and took 3400 before its
+// first operands were read ahead; then, in copies that skip them, they were busy 65% without the tile loads, 77% at
+// 1.81 GHz without LDS reads, 80% without LDS reads and softmax).  LDS reads (256 KB a step) are the next bound, without
+// bank conflicts; the L2 serves 96% of the tile loads.  At head_dim 64, half the products to a softmax: 1.24 to 1.26 ms,
+// 0.89 to 0.90 PFLOP/s.
 // Tried and slower: four wavefronts of 64 rows (half the LDS reads, but 512 registers, half of which only the
 // matrix units address: 3.2 ms); eight without turns at the matrix unit (2.1 ms); row sums by bf16 dot
-// products of two (1.95 against 1.87); asking for the next item before the last steps (2.01 against 1.97).
+// products of two (1.95 against 1.87); asking for the next item before the last steps (2.01 against 1.97); the
+// tile loads with the softmax instead of the products (1.89 against 1.87); equal wave priorities (1.94 against 1.87).
 #pragma once
 
 #include "attn.hpp"
