@@ -536,7 +536,7 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     """Norm of every head of q [N, Hq, D] and k [N, Hkv, D] (where a weight [D] is given) and their rotation by
     positions [N] int32 in one pass (sd_qk_norm_rope).  Rows may be strided (slices of a packed
     projection); inv_freq [R/2] fp32 rotates the first R dims (None: none).  q or k may be None; an output
-    may be its input.  Returns (q_out, k_out)."""
+    may be its input, a new one belongs to the call's stream.  Returns (q_out, k_out)."""
     interleaved = bool(interleaved)
     key = ("rope", eps, interleaved, rot_scale,
            _metas(q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out))
@@ -618,8 +618,9 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      max_ctx: int, max_chunk: int, scale: float = 0.0, out: Optional[torch.Tensor] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
-    without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  Without a
-    workspace a buffer of the stream's and the host thread's is used; a captured call needs its own."""
+    without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  A new output
+    belongs to the call's stream.  Without a workspace a buffer of the stream's and the host thread's is used; a
+    captured call needs its own."""
     key = ("chunk", int(max_ctx), int(max_chunk), float(scale),
            _metas(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, out, workspace))
     c = _call_cache.get(key)
