@@ -522,7 +522,7 @@ def _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved,
         _shape(inv_freq, "inv_freq", None)
         _need(inv_freq, "inv_freq", torch.float32, dev)
     sh = SdRopeShape(0, N, 0, 0, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved),
-                     _dtype_code(x), float(eps), float(rot_scale))
+                     _dtype_code(x), eps, rot_scale)
     _rope_pair(sh, q, q_weight, q_out, "q", dt, dev, N, D)
     _rope_pair(sh, k, k_weight, k_out, "k", dt, dev, N, D)
     return sh
@@ -537,7 +537,7 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     positions [N] int32 in one pass (sd_qk_norm_rope).  Rows may be strided (slices of a packed
     projection); inv_freq [R/2] fp32 rotates the first R dims (None: none).  q or k may be None; an output
     may be its input, a new one belongs to the call's stream.  Returns (q_out, k_out)."""
-    interleaved = bool(interleaved)
+    eps, interleaved, rot_scale = float(eps), bool(interleaved), float(rot_scale)
     key = ("rope", eps, interleaved, rot_scale,
            _metas(q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out))
     c = _call_cache.get(key)
@@ -575,7 +575,7 @@ def _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_of
         _need(inv_freq, "inv_freq", torch.float32, dev)
     _norm_weight(k_weight, "k_weight", k_new)
     sh = SdRopeShape(S, N, 0, Hkv, D, 0 if inv_freq is None else 2 * inv_freq.shape[0], int(interleaved),
-                     _dtype_code(k_pages), float(eps), float(rot_scale), 0, ks, vs)
+                     _dtype_code(k_pages), eps, rot_scale, 0, ks, vs)
     _rope_pair(sh, q, q_weight, q_out, "q", dt, dev, N, D)
     return sh
 
@@ -588,7 +588,7 @@ def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: 
                          q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
     """qk_norm_rope at positions ctx_s + i, with k and v written into page pools [num_pages, Hkv, page_size, D]
     through block_table [S, max_pages] (sd_kv_append_rope_paged).  q may be None (append only).  Returns q_out."""
-    interleaved = bool(interleaved)
+    eps, interleaved, rot_scale = float(eps), bool(interleaved), float(rot_scale)
     key = ("append", eps, interleaved, rot_scale,
            _metas(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight, k_weight, q_out))
     c = _call_cache.get(key)
