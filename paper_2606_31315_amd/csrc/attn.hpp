@@ -557,7 +557,8 @@ __global__ __launch_bounds__(256) void block_attn_merge_kernel(AttnArgs a) {
     }
 #pragma unroll
     for (int k = 0; k < SB; ++k) {
-      if (s0 + k >= nsplit || ml[k].x == -INFINITY) continue;  // a split with no visible key
+      // a split with no visible key (one whose scores are no numbers has no reference either, but a sum that is none)
+      if (s0 + k >= nsplit || (ml[k].x == -INFINITY && ml[k].y == 0.f)) continue;
       const float mn = fmaxf(mx, ml[k].x);
       const float wo = (mx == -INFINITY) ? 0.f : fast_exp2(mx - mn);
       const float wn = fast_exp2(ml[k].x - mn);

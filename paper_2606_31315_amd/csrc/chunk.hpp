@@ -851,7 +851,8 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
       f32x4 o[NVEC];
 #pragma unroll
       for (int v = 0; v < NVEC; ++v) o[v] = po[(size_t)k * (kChunkRows * D / 4) + v * 64];
-      if (x.x == -INFINITY) continue;  // a piece with no visible key
+      // a piece with no visible key (one whose scores are no numbers has no reference either, but a sum that is none)
+      if (x.x == -INFINITY && x.y == 0.f) continue;
       const float mn = fmaxf(mx, x.x), wo = mx == -INFINITY ? 0.f : fast_exp2(mx - mn), wn = fast_exp2(x.x - mn);
       lsum = lsum * wo + x.y * wn;
 #pragma unroll
