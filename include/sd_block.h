@@ -212,8 +212,8 @@ int sd_kv_append_rope_paged(const sd_rope_shape *shape, int32_t page_size, int32
                             const void *q_weight, const void *k_weight, void *q_out, void *k_pages, void *v_pages,
                             void *stream);
 
-/* Workspace bytes sd_chunk_attn_paged needs for this shape (host-only): up to about 135 MB at D = 128 where tiles of
-   query rows may be cut into pieces of keys, a few KB otherwise. */
+/* Workspace bytes sd_chunk_attn_paged needs for this shape (host-only): at most 137 MB at D = 128 and 70 MB at D = 64, and
+   48 bytes for each sequence and 4 for each kv head of one. */
 int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
 
 /*

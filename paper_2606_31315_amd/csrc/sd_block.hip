@@ -172,7 +172,7 @@ int attn_plan(const sd_attn_shape *sh, AttnPlan *p) {
     const long long wmax = sdb::kBalWeightMax8 + 4 * std::max(0LL, nmt_max - 8);
     if (pairs * ((max_L + kBf16KT - 1) / kBf16KT * wmax + sdb::kBalPairCost) > (1LL << 30)) p->bal = 0;
   }
-  const long long slots = p->bal ? std::max(nw, (long long)kBalGrid + pairs) : nw;
+  const long long slots = p->bal ? (long long)kBalGrid + pairs : nw;
   const int nmt = p->Mpad / 16;
   p->MT = nmt <= 8 ? 1 : 2;  // bf16: 8 wavefronts, 1 or 2 m-tiles each
   p->ve = sh->dtype == SD_BF16 && nmt >= 7 && nmt <= 8;
@@ -752,13 +752,15 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   p->off_o = align256(p->off_ml + sizeof(float2) * sdb::kChunkRows * p->slots);
   p->total = p->off_o + sizeof(float) * sdb::kChunkRows * sh->head_dim * p->slots;
   if (p->block) {
-    // They are planned for the longest ctx_s + B_s, max_ctx + max_block; here max_kv_len bounds it too.
+    // They are planned for the longest ctx_s + B_s, max_ctx + max_block; here max_kv_len bounds it too.  Their workspace
+    // grows with the sequences (a slot per pair and per workgroup): past the bound of the chunk kernel's, that kernel takes
+    // the call (32 rows of 256 sequences at 8192 keys, 8 kv heads: 1852 us there, 1673 here).
     p->block_sh = *sh;
     p->block_sh.max_ctx = std::min(sh->max_ctx, sh->max_kv_len - sh->max_block);
     AttnPlan ap;
-    rc = attn_plan(&p->block_sh, &ap);
-    if (rc) return rc;
-    p->total = ap.total;
+    const size_t most_bytes = (size_t)sdb::kChunkSlots * sdb::kChunkRows * (sizeof(float) * sh->head_dim + sizeof(float2));
+    p->block = attn_plan(&p->block_sh, &ap) == SD_OK && ap.total <= most_bytes;
+    if (p->block) p->total = ap.total;
   }
   return ok();
 }
