@@ -257,6 +257,7 @@ class StreamWorkspace(threading.local):
         key = (device.index, _stream(None))
         buf = self._bufs.get(key)
         if buf is None or buf.numel() < nbytes:
+            buf = self._bufs[key] = None  # given back first: its memory may serve the larger one
             buf = self._bufs[key] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
         return buf
 

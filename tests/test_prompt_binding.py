@@ -1,6 +1,7 @@
 """The binding of the calls that put a prompt into a paged cache, on the CPU: tensors that say they are on a device, a
 library that notes what it is asked for."""
 import types
+import weakref
 
 import pytest
 import torch
@@ -66,3 +67,22 @@ def test_numbers_in_tensors_are_read_at_each_call(asked, call, name):
     x.fill_(0.5)
     call(**{name: x})
     assert [f[name] for _, f in asked] == [0.25, 0.5]
+
+
+def test_a_workspace_that_is_grown_out_of_is_given_back_first(monkeypatch):
+    empty, held, sizes = torch.empty, [], []
+
+    def make(n, device=None, **k):
+        assert not held or held[-1]() is None, "the smaller buffer is still held"
+        sizes.append(n)
+        buf = empty(n, **k)
+        held.append(weakref.ref(buf))
+        return buf
+
+    monkeypatch.setattr(torch, "empty", make)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(L, "_stream", lambda stream: 5)
+    ws, cuda = L.StreamWorkspace(), torch.device("cuda", 0)
+    for n in (1000, 5000, 3000, 9000):
+        assert ws.get(n, cuda, None).numel() >= n
+    assert sizes == [1000, 5000, 9000]
