@@ -290,6 +290,18 @@ def _cached_call(key, make_shape, nbytes):
     return c
 
 
+# The prompt calls' own table: their rows and bounds change from one call to the next, and a table shared with the
+# per-step calls would be cleared under those.
+_prompt_cache: dict = {}
+
+
+def _cached_prompt_call(key, shape, nbytes: int = 0):
+    if len(_prompt_cache) >= _CALL_CACHE_MAX:
+        _prompt_cache.clear()
+    c = _prompt_cache[key] = (shape, ctypes.byref(shape), nbytes)
+    return c
+
+
 def attn_workspace_size(shape: SdAttnShape) -> int:
     n = ctypes.c_size_t(0)
     _check(lib().sd_block_attn_workspace_size(ctypes.byref(shape), ctypes.byref(n)))
@@ -541,10 +553,10 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
     eps, interleaved, rot_scale = float(eps), bool(interleaved), float(rot_scale)
     key = ("rope", eps, interleaved, rot_scale,
            _metas(q, k, positions, inv_freq, q_weight, k_weight, q_out, k_out))
-    c = _call_cache.get(key)
+    c = _prompt_cache.get(key)
     if c is None:
         sh = _rope_shape(q, k, positions, inv_freq, q_weight, k_weight, eps, interleaved, rot_scale, q_out, k_out)
-        c = _cached_call(key, lambda: sh, lambda _: 0)
+        c = _cached_prompt_call(key, sh)
     _on_current(positions, stream)
     if q_out is None and q is not None:
         q_out = _new_like(q, stream)
@@ -592,11 +604,11 @@ def kv_append_rope_paged(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: 
     eps, interleaved, rot_scale = float(eps), bool(interleaved), float(rot_scale)
     key = ("append", eps, interleaved, rot_scale,
            _metas(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight, k_weight, q_out))
-    c = _call_cache.get(key)
+    c = _prompt_cache.get(key)
     if c is None:
         sh = _append_shape(q, k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets, inv_freq, q_weight,
                            k_weight, eps, interleaved, rot_scale, q_out)
-        c = _cached_call(key, lambda: sh, lambda _: 0)
+        c = _cached_prompt_call(key, sh)
     _on_current(k_pages, stream)
     if q_out is None and q is not None:
         q_out = _new_like(q, stream)
@@ -624,12 +636,12 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
     captured call needs its own."""
     key = ("chunk", int(max_ctx), int(max_chunk), float(scale),
            _metas(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, out, workspace))
-    c = _call_cache.get(key)
+    c = _prompt_cache.get(key)
     if c is None:
         if workspace is not None:
             _need(workspace, "workspace", None, k_pages.device if isinstance(k_pages, torch.Tensor) else None)
         sh = _chunk_shape(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, max_ctx, max_chunk, scale, out)
-        c = _cached_call(key, lambda: sh, chunk_attn_workspace_size)
+        c = _cached_prompt_call(key, sh, chunk_attn_workspace_size(sh))
     _, ref, nbytes = c
     _on_current(q, stream)
     if out is None:

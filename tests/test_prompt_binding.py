@@ -45,6 +45,7 @@ def asked(monkeypatch):
     monkeypatch.setattr(L, "_cur_device", lambda: 0)
     monkeypatch.setattr(L, "_raw_stream", lambda device: 5)
     monkeypatch.setattr(L, "_call_cache", {})
+    monkeypatch.setattr(L, "_prompt_cache", {}, raising=False)
     return out
 
 
@@ -86,3 +87,14 @@ def test_a_workspace_that_is_grown_out_of_is_given_back_first(monkeypatch):
     for n in (1000, 5000, 3000, 9000):
         assert ws.get(n, cuda, None).numel() >= n
     assert sizes == [1000, 5000, 9000]
+
+
+def test_prompts_of_many_lengths_leave_the_per_step_calls_entries(asked):
+    """The table of the per-step calls is cleared when it is full: the prompt calls do not fill it."""
+    keep = L._call_cache["attn"] = object()
+    pool, table, lens, off, ws = dev(9, 2, 16, 128), dev(3, 4, dt=I32), dev(3, dt=I32), dev(4, dt=I32), dev(1 << 22, dt=torch.uint8)
+    for n in range(2 * L._CALL_CACHE_MAX):
+        L.chunk_attn_paged(dev(1 + n % 8, 4, 128), pool, pool, table, lens, lens, off, 0, max_ctx=n % 60, max_chunk=3 + n // 60,
+                           workspace=ws)
+        _rope(eps=float(n))
+    assert L._call_cache == {"attn": keep} and len(L._prompt_cache) <= L._CALL_CACHE_MAX
