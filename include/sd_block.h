@@ -28,7 +28,8 @@
  *     returns a status code; it never aborts or prints.  Per-sequence values that
  *     live in device memory (ctx_lens, block_lens, q_offsets, tokens) cannot be
  *     checked on the host: values outside the documented ranges are undefined
- *     behaviour (sd_check_attn_inputs and sd_check_accept_inputs test them on the device).
+ *     behaviour (sd_check_attn_inputs, sd_check_chunk_inputs and sd_check_accept_inputs test
+ *     them on the device).
  *   - Workspace: each operation needs device scratch memory of the size its
  *     *_workspace_size() reports (partial results between the kernels of one
  *     call).  Its contents on entry do not matter.  Calls that share a workspace
@@ -364,6 +365,15 @@ enum {
  */
 int sd_check_attn_inputs(const sd_attn_shape *shape, const int32_t *ctx_lens, const int32_t *block_lens,
                          const int32_t *q_offsets, int32_t *status, void *stream);
+
+/*
+ * The same for sd_chunk_attn_paged: chunk_lens in [0, max_block], ctx_lens in [0, max_ctx], ctx_s + B_s <= max_kv_len
+ * (SD_CHECK_CTX) and q_offsets an exclusive prefix sum that ends at total_q or before it.  max_kv_len of the shape is used
+ * too; max_ctx and max_block are bounded as there.
+ * Errors: SD_ERR_INVALID_ARG, SD_ERR_HIP.
+ */
+int sd_check_chunk_inputs(const sd_attn_shape *shape, const int32_t *ctx_lens, const int32_t *chunk_lens,
+                          const int32_t *q_offsets, int32_t *status, void *stream);
 
 /*
  * The same for sd_accept: block_lens, q_offsets, draft_tokens [total_q - S] and, when

@@ -23,7 +23,7 @@ EXPORTS = ["sd_last_error", "sd_version", "sd_block_attn_workspace_size", "sd_bl
            "sd_accept_workspace_size", "sd_accept", "sd_kv_append", "sd_commit", "sd_verify_step_workspace_size",
            "sd_verify_step", "sd_policy_workspace_size", "sd_block_size_policy", "sd_block_attn_paged",
            "sd_kv_append_paged", "sd_survival_tau", "sd_survival_sample", "sd_block_attn_append",
-           "sd_check_attn_inputs", "sd_check_accept_inputs", "sd_accept_noalloc", "sd_accept_set_path",
+           "sd_check_attn_inputs", "sd_check_chunk_inputs", "sd_check_accept_inputs", "sd_accept_noalloc", "sd_accept_set_path",
            "sd_qk_norm_rope", "sd_kv_append_rope_paged", "sd_chunk_attn_workspace_size", "sd_chunk_attn_paged"]
 
 # bytes of the fixed device scratch behind sd_accept_noalloc (SD_ACCEPT_NOALLOC_SCRATCH_BYTES)
@@ -125,6 +125,8 @@ def lib() -> ctypes.CDLL:
         L.sd_survival_sample.argtypes = [ctypes.POINTER(SdSurvivalShape), P, ctypes.c_uint64, I, P, P, P]
         L.sd_check_attn_inputs.restype = ctypes.c_int
         L.sd_check_attn_inputs.argtypes = [ctypes.POINTER(SdAttnShape), P, P, P, P, P]
+        L.sd_check_chunk_inputs.restype = ctypes.c_int
+        L.sd_check_chunk_inputs.argtypes = [ctypes.POINTER(SdAttnShape), P, P, P, P, P]
         L.sd_accept_set_path.restype = ctypes.c_int
         L.sd_accept_set_path.argtypes = [I, I]
         L.sd_check_accept_inputs.restype = ctypes.c_int
@@ -799,6 +801,18 @@ def accept_set_path(mode: int, spin_limit: int = 0) -> None:
     _check(lib().sd_accept_set_path(int(mode), int(spin_limit)))
 
 
+def _check_lens(call: str, shape: SdAttnShape, lens_name: str, lens, ctx_lens, q_offsets, status, stream) -> torch.Tensor:
+    dev = lens.device
+    for name, t in (("ctx_lens", ctx_lens), (lens_name, lens), ("q_offsets", q_offsets)):
+        _need(t, name, torch.int32, dev)
+    if status is None:
+        status = torch.empty(3, dtype=torch.int32, device=dev)
+    _need(status, "status", torch.int32, dev)
+    _check(getattr(lib(), call)(ctypes.byref(shape), _ptr(ctx_lens), _ptr(lens), _ptr(q_offsets), _ptr(status),
+                                _stream(stream)))
+    return status
+
+
 def check_attn_inputs(ctx_lens: torch.Tensor, block_lens: torch.Tensor, q_offsets: torch.Tensor, *, total_q: int,
                       max_ctx: int, max_block: int, status: Optional[torch.Tensor] = None,
                       stream=None) -> torch.Tensor:
@@ -808,18 +822,25 @@ def check_attn_inputs(ctx_lens: torch.Tensor, block_lens: torch.Tensor, q_offset
     _lens_shapes(block_lens.shape[0], ctx_lens=ctx_lens, q_offsets=q_offsets)
     if status is not None:
         _shape(status, "status", 3)
-    dev = block_lens.device
-    for name, t in (("ctx_lens", ctx_lens), ("block_lens", block_lens), ("q_offsets", q_offsets)):
-        _need(t, name, torch.int32, dev)
-    if status is None:
-        status = torch.empty(3, dtype=torch.int32, device=dev)
-    _need(status, "status", torch.int32, dev)
     shape = SdAttnShape(num_seqs=block_lens.shape[0], num_q_heads=1, num_kv_heads=1, head_dim=128,
                         max_kv_len=max_ctx + max_block, total_q=total_q, max_ctx=max_ctx, max_block=max_block,
                         dtype=SD_BF16, scale=0.0)
-    _check(lib().sd_check_attn_inputs(ctypes.byref(shape), _ptr(ctx_lens), _ptr(block_lens), _ptr(q_offsets),
-                                      _ptr(status), _stream(stream)))
-    return status
+    return _check_lens("sd_check_attn_inputs", shape, "block_lens", block_lens, ctx_lens, q_offsets, status, stream)
+
+
+def check_chunk_inputs(ctx_lens: torch.Tensor, chunk_lens: torch.Tensor, q_offsets: torch.Tensor, *, total_q: int,
+                       max_ctx: int, max_chunk: int, max_kv_len: int, status: Optional[torch.Tensor] = None,
+                       stream=None) -> torch.Tensor:
+    """sd_check_chunk_inputs: the same for the lengths of chunk_attn_paged; max_kv_len is the keys that a sequence's row
+    of the block table holds."""
+    _shape(chunk_lens, "chunk_lens", None)
+    _lens_shapes(chunk_lens.shape[0], ctx_lens=ctx_lens, q_offsets=q_offsets)
+    if status is not None:
+        _shape(status, "status", 3)
+    shape = SdAttnShape(num_seqs=chunk_lens.shape[0], num_q_heads=1, num_kv_heads=1, head_dim=128,
+                        max_kv_len=max_kv_len, total_q=total_q, max_ctx=max_ctx, max_block=max_chunk,
+                        dtype=SD_BF16, scale=0.0)
+    return _check_lens("sd_check_chunk_inputs", shape, "chunk_lens", chunk_lens, ctx_lens, q_offsets, status, stream)
 
 
 def check_accept_inputs(draft_tokens: torch.Tensor, uniforms: Optional[torch.Tensor], block_lens: torch.Tensor,

@@ -11,9 +11,9 @@
 namespace sdb {
 
 enum : int {
-  kCheckCtx = 1,       // ctx_s outside [0, max_ctx]
+  kCheckCtx = 1,       // ctx_s outside [0, max_ctx], or ctx_s + B_s past max_keys
   kCheckBlock = 2,     // B_s outside [min_block, max_block]
-  kCheckOffsets = 4,   // q_offsets not the exclusive prefix sum of block_lens ending at total_q
+  kCheckOffsets = 4,   // q_offsets not the exclusive prefix sum of block_lens ending at total_q (padded: at most there)
   kCheckToken = 8,     // a drafted token outside [0, V)
   kCheckUniform = 16,  // a uniform outside [0, 1) (NaN included)
 };
@@ -26,6 +26,7 @@ struct CheckArgs {
   const float *uniforms;    // [total_q] or null (attention, or acceptance at T = 0)
   int *status;              // [3]: OR of the bits, first offending sequence or -1, count
   int S, total_q, max_ctx, min_block, max_block, vocab;
+  int max_keys, padded;     // attention of chunks; else INT_MAX, 0
 };
 
 __global__ __launch_bounds__(256) void check_inputs_kernel(CheckArgs a) {
@@ -44,10 +45,10 @@ __global__ __launch_bounds__(256) void check_inputs_kernel(CheckArgs a) {
     if (B < a.min_block || B > a.max_block) e |= kCheckBlock;
     if (a.ctx_lens) {
       const int c = a.ctx_lens[s];
-      if (c < 0 || c > a.max_ctx) e |= kCheckCtx;
+      if (c < 0 || c > a.max_ctx || (B <= a.max_block && (long long)c + B > a.max_keys)) e |= kCheckCtx;
     }
     const int o0 = a.q_offsets[s], o1 = a.q_offsets[s + 1];
-    if ((s == 0 && o0 != 0) || (s == a.S - 1 && o1 != a.total_q) || o1 - o0 != B || o0 < 0 || o1 > a.total_q)
+    if ((s == 0 && o0 != 0) || (s == a.S - 1 && !a.padded && o1 != a.total_q) || o1 - o0 != B || o0 < 0 || o1 > a.total_q)
       e |= kCheckOffsets;
     if (!(e & (kCheckBlock | kCheckOffsets))) {  // rows [o0, o1) lie inside [0, total_q)
       if (a.draft_tokens) {

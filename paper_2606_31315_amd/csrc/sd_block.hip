@@ -1275,13 +1275,12 @@ static_assert(SD_CHECK_CTX == sdb::kCheckCtx && SD_CHECK_BLOCK == sdb::kCheckBlo
                   SD_CHECK_UNIFORM == sdb::kCheckUniform,
               "check bits of the header and the kernel agree");
 
-int sd_check_attn_inputs(const sd_attn_shape *sh, const int32_t *ctx_lens, const int32_t *block_lens,
-                         const int32_t *q_offsets, int32_t *status, void *stream) {
-  if (!sh) return fail(SD_ERR_INVALID_ARG, "sd_check_attn_inputs: shape is NULL");
-  if (sh->num_seqs < 0 || sh->total_q < 0 || sh->max_ctx < 0 || sh->max_block < 1 || sh->max_block > 64)
-    return fail(SD_ERR_INVALID_ARG, "sd_check_attn_inputs: num_seqs, total_q, max_ctx or max_block out of range");
+namespace {
+
+int check_attn_lens(const char *what, const sd_attn_shape *sh, int max_keys, bool padded, const int32_t *ctx_lens,
+                    const int32_t *block_lens, const int32_t *q_offsets, int32_t *status, void *stream) {
   if (!status || (sh->num_seqs > 0 && (!ctx_lens || !block_lens || !q_offsets)))
-    return fail(SD_ERR_INVALID_ARG, "sd_check_attn_inputs: NULL pointer argument");
+    return fail(SD_ERR_INVALID_ARG, "%s: NULL pointer argument", what);
   sdb::CheckArgs a{};
   a.ctx_lens = ctx_lens;
   a.block_lens = block_lens;
@@ -1292,8 +1291,29 @@ int sd_check_attn_inputs(const sd_attn_shape *sh, const int32_t *ctx_lens, const
   a.max_ctx = sh->max_ctx;
   a.min_block = 0;
   a.max_block = sh->max_block;
+  a.max_keys = max_keys;
+  a.padded = padded;
   hipLaunchKernelGGL(sdb::check_inputs_kernel, dim3(1), dim3(256), 0, (hipStream_t)stream, a);
-  return check_launch("sd_check_attn_inputs");
+  return check_launch(what);
+}
+
+}  // namespace
+
+int sd_check_attn_inputs(const sd_attn_shape *sh, const int32_t *ctx_lens, const int32_t *block_lens,
+                         const int32_t *q_offsets, int32_t *status, void *stream) {
+  if (!sh) return fail(SD_ERR_INVALID_ARG, "sd_check_attn_inputs: shape is NULL");
+  if (sh->num_seqs < 0 || sh->total_q < 0 || sh->max_ctx < 0 || sh->max_block < 1 || sh->max_block > 64)
+    return fail(SD_ERR_INVALID_ARG, "sd_check_attn_inputs: num_seqs, total_q, max_ctx or max_block out of range");
+  return check_attn_lens("sd_check_attn_inputs", sh, INT_MAX, false, ctx_lens, block_lens, q_offsets, status, stream);
+}
+
+int sd_check_chunk_inputs(const sd_attn_shape *sh, const int32_t *ctx_lens, const int32_t *chunk_lens,
+                          const int32_t *q_offsets, int32_t *status, void *stream) {
+  if (!sh) return fail(SD_ERR_INVALID_ARG, "sd_check_chunk_inputs: shape is NULL");
+  if (sh->num_seqs < 0 || sh->total_q < 0 || sh->max_kv_len < 1 || sh->max_ctx < 0 || sh->max_ctx > sh->max_kv_len ||
+      sh->max_block < 1 || sh->max_block > sh->max_kv_len)
+    return fail(SD_ERR_INVALID_ARG, "sd_check_chunk_inputs: num_seqs, total_q, max_kv_len, max_ctx or max_block out of range");
+  return check_attn_lens("sd_check_chunk_inputs", sh, sh->max_kv_len, true, ctx_lens, chunk_lens, q_offsets, status, stream);
 }
 
 int sd_check_accept_inputs(const sd_accept_shape *sh, const int32_t *draft_tokens, const float *uniforms,
@@ -1317,6 +1337,7 @@ int sd_check_accept_inputs(const sd_accept_shape *sh, const int32_t *draft_token
   a.min_block = 1;
   a.max_block = sh->max_block;
   a.vocab = sh->vocab;
+  a.max_keys = INT_MAX;
   hipLaunchKernelGGL(sdb::check_inputs_kernel, dim3(1), dim3(256), 0, (hipStream_t)stream, a);
   return check_launch("sd_check_accept_inputs");
 }
