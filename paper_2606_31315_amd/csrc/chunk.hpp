@@ -192,8 +192,9 @@ struct ChunkTile {
   __device__ static int swz_v(int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
 };
 
+// A context below 0, which no caller may give, counts as 0: no read lies before the sequence's row of the block table.
 __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs &a, int s) {
-  return ChunkSeq{a.ctx_lens[s], a.chunk_lens[s], a.P, a.G, a.causal};
+  return ChunkSeq{max(a.ctx_lens[s], 0), a.chunk_lens[s], a.P, a.G, a.causal};
 }
 
 // The plan, by one workgroup.  Sums of work are whole numbers in doubles and every order is fixed: the same lengths
@@ -362,15 +363,15 @@ __device__ __forceinline__ bool chunk_tile(const ChunkArgs &a, int b, ChunkEntry
   int before = 0;
   for (int c0 = 0; c0 < a.S; c0 += 64) {
     const int k = min(c0 + lane, a.S - 1);  // clamped: no per-load branch
-    const int ctx = a.ctx_lens[k], B = a.chunk_lens[k], off = a.q_offsets[k];
-    const int nt = c0 + lane < a.S ? ChunkSeq{ctx, B, a.P, a.G, a.causal}.tiles() : 0;
+    const ChunkSeq q = chunk_seq(a, k);
+    const int off = a.q_offsets[k], nt = c0 + lane < a.S ? q.tiles() : 0;
     const int items = nt * a.Hkv, incl = before + wave_scan_i(items);
     const unsigned long long hit = __ballot(incl > b && incl - items <= b);
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;  // wave-uniform
       e.s = c0 + l;
-      e.ctx = __builtin_amdgcn_readlane(ctx, l);
-      e.B = __builtin_amdgcn_readlane(B, l);
+      e.ctx = __builtin_amdgcn_readlane(q.ctx, l);
+      e.B = __builtin_amdgcn_readlane(q.B, l);
       e.qoff = __builtin_amdgcn_readlane(off, l);
       const int n = __builtin_amdgcn_readlane(nt, l), r = b - __builtin_amdgcn_readlane(incl - items, l);
       g = r / n;

@@ -34,3 +34,14 @@ def test_keys_that_are_no_numbers_reach_every_row(ctx, B, first, keys, D):
     pages = b["table"][0, first // 64:(first + keys) // 64].long()
     b["kp"][pages] = float("nan")
     assert bool(_run(b, CAUSAL).isnan().all())
+
+
+@pytest.mark.parametrize("ctx", [[40, 90], [40, 9000]], ids=["one_launch", "planned"])
+def test_a_context_below_zero_reads_nothing_before_its_table(ctx):
+    """Lengths that the contract forbids: the sequence counts as one without a context, the other as it is."""
+    b = R.chunk_batch(51, 16, 8, 128, 16, ctx, [70, 80], G.dev())
+    most = max(ctx)
+    b["ctx"][0] = -40
+    got = _run(b, CAUSAL, max_ctx=most)
+    b["ctx"][0] = 0
+    R.assert_attended(got, b["q"], b["kp"], b["vp"], b["table"], b["ctx"], b["B"], b["off"], CAUSAL)
