@@ -120,6 +120,36 @@ SDB_HD int chunk_piece(int n, int np, int i) {
   return i == np ? n : (int)(steps * i / np) * kChunkKT;
 }
 
+#if defined(__HIPCC__)
+#define SDB_UNROLL4 _Pragma("unroll 4")
+#else
+#define SDB_UNROLL4
+#endif
+// The order of the sequences: those of few rows, which memory bounds, and the others, which the products bound, each kind
+// longest first, the two interleaved by the share of their work that is done by then.
+// A sequence's length, its kind marked by the sign.
+SDB_HD float chunk_key(const ChunkSeq &q) { return (float)q.longest() * (q.few() ? -1.f : 1.f); }
+// Share of its kind's work done when sequence t is half done, from all keys and units of work.
+SDB_HD float chunk_place(const float *key, const float *work, int S, int t) {
+  const float k = key[t];
+  float before = 0.f, all = 0.f;
+  SDB_UNROLL4
+  for (int i = 0; i < S; ++i) {
+    const float u = key[i], au = u < 0.f ? -u : u, ak = k < 0.f ? -k : k, w = (u < 0.f) == (k < 0.f) ? work[i] : 0.f;
+    all += w;
+    before += au > ak || (u == k && i < t) ? w : 0.f;
+  }
+  return all > 0.f ? (before + 0.5f * work[t]) / all : 2.f;  // sequences without rows come last
+}
+// Its rank by these.
+SDB_HD int chunk_rank(const float *place, int S, int t) {
+  const float at = place[t];
+  int rank = 0;
+  SDB_UNROLL4
+  for (int i = 0; i < S; ++i) rank += place[i] < at || (place[i] == at && i < t);
+  return rank;
+}
+
 // What the plan says of a sequence, in the order of the queues.
 struct ChunkEntry {
   int s, ctx, B, qoff;
@@ -207,14 +237,14 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
   __shared__ double sums[kChunkPlanThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, S = a.S;
   const bool sorted = S <= kChunkSortSeqs;
-  // the batch's work; sequences by their longest tile, those of few rows marked by the sign
+  // the batch's work, and the order
   double mine = 0;
   float k = 0.f, work = 0.f;
   for (int s = tid; s < S; s += kChunkPlanThreads) {
     const ChunkSeq q = chunk_seq(a, s);
     const double u = q.all_units();
     mine += u * a.Hkv;
-    k = (float)q.longest() * (q.few() ? -1.f : 1.f);
+    k = chunk_key(q);
     work = (float)u;
   }
   if (tid < kChunkSortSeqs) key[tid] = k, place[tid] = work;
@@ -224,26 +254,11 @@ __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs
   double total = 0;
   for (int w = 0; w < kChunkPlanThreads / 64; ++w) total += sums[w];
   if (sorted) {
-    // Each kind longest first, and the two interleaved by the share of their work that is done by then.
-    float before = 0.f, all = 0.f;
-    if (tid < S) {
-#pragma unroll 4
-      for (int t = 0; t < S; ++t) {
-        const float u = key[t], w = (u < 0.f) == (k < 0.f) ? place[t] : 0.f;
-        all += w;
-        before += fabsf(u) > fabsf(k) || (u == k && t < tid) ? w : 0.f;
-      }
-    }
-    const float at = all > 0.f ? (before + 0.5f * work) / all : 2.f;  // sequences without rows come last
+    const float at = tid < S ? chunk_place(key, place, S, tid) : 0.f;
     __syncthreads();
     if (tid < S) place[tid] = at;
     __syncthreads();
-    if (tid < S) {
-      int rank = 0;
-#pragma unroll 4
-      for (int t = 0; t < S; ++t) rank += place[t] < at || (place[t] == at && t < tid);
-      order[rank] = tid;
-    }
+    if (tid < S) order[chunk_rank(place, S, tid)] = tid;
   }
   __syncthreads();
   // entries from the last to the first, 64 a round: what lies behind each is known then
