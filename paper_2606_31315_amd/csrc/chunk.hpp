@@ -408,9 +408,9 @@ constexpr float kChunkSum = 4096.f;
 // after the builtin; the waits are chunk_phase_end's.  (Its own waits for vector loads count the transfers
 // as well, so they only grow stricter.)  The five wait states are those between a lane read that may
 // have written the base and a vector load from it, which the compiler sees to only for its own.
-// Nothing else in these kernels uses m0.
 __device__ __forceinline__ void chunk_load_lds(const char *base, unsigned off, unsigned dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(off), "s"(base)
+               : "m0", "memory");
 }
 
 // Ends a phase: this wavefront's LDS reads are done, and all but its N youngest transfers (N < 0: no
