@@ -55,9 +55,13 @@ constexpr int kChunkSpread = 64;      // else a tile is cut where less than this
 constexpr int kChunkEndPieces = 3;    // into this many pieces
 constexpr int kChunkPieceExtra = 512; // keys' worth of cutting: sums filed and joined
 
-// Relative time of a key by the tile's rows (a step of 256 rows takes 3390 cycles, of 128 2720, of 64 2590).  Those
-// of sequences of few rows are bound by memory, and by less of it the more of them run at once.
-SDB_HD int chunk_weight(int rows, bool few = false) { return plan_max((rows + 31) / 32, few ? 3 : 5); }
+// Relative time of a key by the tile's rows.  A step of few rows still goes through both phases and their barriers: 1024
+// tiles over the same 4096 keys take 509 us with 256 rows, 438 with 192, 357 with 128, 335 with 64 and 320 with 4, that is
+// 8 : 6.9 : 5.6 : 5.3 : 5.0 (head_dim 64: 326, 295, 268, 252, 239); with keys of their own 604, 533, 445, 414, 397.  With 6 for
+// the least, batches take the same (400 rows at 4000 keys 50.8 and 50.9 us, prompt chunks of 200 to 900 rows beside single
+// tokens of 64 sequences 1134 and 1137); with 3 for sequences of few rows, too (1138 and 1134; at head_dim 64, 16
+// sequences, 192 and 200).
+SDB_HD int chunk_weight(int rows) { return plan_max((rows + 31) / 32, 5); }
 
 struct ChunkSeq {
   int ctx, B, P, G, causal;
@@ -65,7 +69,7 @@ struct ChunkSeq {
   SDB_HD int rows(int j) const { return plan_min(P, B - P * j) * G; }           // of tile j
   SDB_HD int keys(int j) const { return ctx + (causal ? plan_min(P * (j + 1), B) : B); }
   // Work of tile j, and of the tiles before it (which are all full): whole numbers, below 2^53 (the host checks).
-  SDB_HD double units(int j) const { return (double)chunk_weight(rows(j), few()) * ((double)keys(j) + kChunkPieceCost); }
+  SDB_HD double units(int j) const { return (double)chunk_weight(rows(j)) * ((double)keys(j) + kChunkPieceCost); }
   SDB_HD double before(int j) const {
     const double n = j, each = (double)(causal ? ctx : ctx + B) + kChunkPieceCost;
     return chunk_weight(P * G) * (n * each + (causal ? n * (n + 1) / 2 * P : 0));

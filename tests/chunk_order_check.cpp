@@ -110,7 +110,7 @@ extern "C" int check_order(int S, int Hkv, int G, int causal, const int *ctx, co
         NEED(k0 == at[j] && k1 >= k0);  // a tile's pieces follow one another in the queue
         at[j] = k1;
         keys += k1 - k0;
-        const double w = (double)chunk_weight(q.rows(j), q.few()) * (k1 - k0 + kChunkPieceCost);
+        const double w = (double)chunk_weight(q.rows(j)) * (k1 - k0 + kChunkPieceCost);
         if (w > *longest_out) *longest_out = w;
         if (p >= 0) {
           const int sl = e.slot(g, j, p);
