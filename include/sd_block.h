@@ -159,6 +159,12 @@ int sd_block_attn_append(const sd_attn_shape *shape, const void *q, const void *
  * make it: norm and position rotation of a chunk's queries and keys, its keys and values into the
  * pages, and the attention of the chunk over what is cached.  A prompt may come in any number of
  * chunks, and chunks of prompts may share a batch with single tokens of other sequences.
+ *
+ * The contiguous caches [S, Hkv, Lmax, D] of sd_block_attn and sd_verify_step are such pools where Lmax
+ * is a page size (a power of two in [16, 4096]): S pages, max_pages 1, block_table[s] = s.  Others are
+ * filled by sd_qk_norm_rope and sd_kv_append, which take any number of rows; over them attention is
+ * sd_block_attn's, 64 rows at a time.  fp32 pages are for such caches: the attention calls over page
+ * pools, sd_chunk_attn_paged among them, are bf16 only.
  * ========================================================================== */
 typedef struct sd_rope_shape {
   int32_t num_seqs;     /* S >= 0 (sd_kv_append_rope_paged; else unused) */
@@ -220,7 +226,8 @@ int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
 /*
  * sd_block_attn_paged for any number of new rows per sequence: shape->max_block bounds chunk_lens.
  * max_ctx and max_block lie in [0, max_kv_len] and [1, max_kv_len], and ctx_s + B_s <= max_kv_len for
- * every s (their bounds' sum may be more), which is at most 2^31 - 513; Hq/Hkv <= 256.
+ * every s (their bounds' sum may be more), which is at most 2^31 - 513; Hq/Hkv <= 256; total_q <= S * max_block.
+ * sd_check_chunk_inputs tests the lengths.
  * Everything else is as there: bf16 page pools that already hold the chunk's keys and values, the masks,
  * fp32 softmax and sums with weights rounded to bf16, asynchronous, no synchronisation.
  *   chunk_lens [S] int32      rows of sequence s, 0 <= B_s <= max_block
@@ -228,9 +235,8 @@ int sd_chunk_attn_workspace_size(const sd_attn_shape *shape, size_t *bytes);
  *                             from q_offsets[S] on are left as they were
  * Where a tile's keys are cut, and so the rounding of its sums, depends on the batch's lengths and the shape; the same
  * call gives the same bits.  Work is handed out through counters in the workspace, which the call sets itself.
- * Keys and values of a sequence at [0, ctx_s + B_s) are finite: a value that is not reaches every row of the
- * tile that holds it, masked for that row or not (0 * inf).  What lies behind ctx_s + B_s in a page is
- * never read.
+ * Keys and values of a sequence at [0, ctx_s + B_s) are finite: a value that is not reaches every row that sees it, and
+ * may reach others of the sequence that do not (0 * inf).  What lies behind ctx_s + B_s in a page is never read.
  * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED (head_dim, group size, dtype), SD_ERR_WORKSPACE,
  * SD_ERR_HIP.  S == 0 or total_q == 0 returns SD_OK without touching the device.
  */

@@ -634,8 +634,8 @@ def chunk_attn_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tens
                      workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of chunks of any number of new rows over paged caches (sd_chunk_attn_paged): block_attn_paged
     without its limit on the rows.  max_ctx and max_chunk are host-known bounds of the device lengths.  A new output
-    belongs to the call's stream.  Without a workspace a buffer of the stream's and the host thread's is used; a
-    captured call needs its own."""
+    belongs to the call's stream.  Without a workspace a buffer of the stream's and the host thread's is used and kept
+    while the thread lives (up to 137 MB); a captured call needs its own."""
     key = ("chunk", int(max_ctx), int(max_chunk), float(scale),
            _metas(q, k_pages, v_pages, block_table, ctx_lens, chunk_lens, q_offsets, out, workspace))
     c = _prompt_cache.get(key)

@@ -15,12 +15,12 @@
 // to key; sums and O stay fp32.
 //
 // Bound, for long chunks, by the matrix cores and the power they draw: 2048 rows at 65536 keys (32 heads on 4) take
-// 1.84 to 1.90 ms from card to card, 1.17 to 1.21 PFLOP/s, where a matrix product of 16384^3 reaches 1.37.  The matrix
+// 1.83 to 1.94 ms from card to card, 1.15 to 1.22 PFLOP/s, where a matrix product of 16384^3 reaches 1.37.  The matrix
 // units are busy 62% of the cycles at a clock of 2.0 GHz (a step is 2048 cycles of products and took 3400 before its
 // first operands were read ahead; then, in copies that skip them, they were busy 65% without the tile loads, 77% at
 // 1.81 GHz without LDS reads, 80% without LDS reads and softmax).  LDS reads (256 KB a step) are the next bound, without
-// bank conflicts; the L2 serves 96% of the tile loads.  At head_dim 64, half the products to a softmax: 1.24 to 1.26 ms,
-// 0.89 to 0.90 PFLOP/s.
+// bank conflicts; the L2 serves 96% of the tile loads.  At head_dim 64, half the products to a softmax: 1.13 to 1.26 ms,
+// 0.89 to 0.99 PFLOP/s.
 // Tried and slower: four wavefronts of 64 rows (half the LDS reads, but 512 registers, half of which only the
 // matrix units address: 3.2 ms); eight without turns at the matrix unit (2.1 ms); row sums by bf16 dot
 // products of two (1.95 against 1.87); asking for the next item before the last steps (2.01 against 1.97); the
@@ -36,7 +36,7 @@ constexpr int kChunkKT = 64;     // keys of a step
 
 // ---- plan --------------------------------------------------------------------------
 // Query tiles have from one key step to thousands, and their number seldom fits the device.  A small
-// launch orders the sequences by their longest tile, longest first, deals their kv heads to eight
+// launch orders the sequences, longest tiles first, deals their kv heads to eight
 // queues, one per XCD, and decides which tiles are cut into pieces of keys: those near the end of the
 // order, whose length the work behind them could not even out.  Workgroups take the next item of
 // their XCD's queue, and of another when that is empty.  The tiles of one kv head are neighbours in a queue, so
@@ -233,6 +233,9 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkArgs &a, int s) {
 
 // The plan, by one workgroup.  Sums of work are whole numbers in doubles and every order is fixed: the same lengths
 // give the same plan.
+// Its order costs two walks over the batch for every sequence, its entries one wavefront's 64 at a time: 5.5 us for one
+// sequence, 9 to 12 for 32, 23 for 128, 43 for 256, 87 for 512, 207 for 1024 (an eighth of such a call: single tokens of
+// nine sequences in ten, contexts of 500 to 2000 keys, 354 us for 256 and 1436 for 1024), 36 for 1025, which are not ordered.
 constexpr int kChunkPlanThreads = 1024;
 static_assert(kChunkSortSeqs <= kChunkPlanThreads, "a thread per sequence");
 __global__ __launch_bounds__(kChunkPlanThreads) void chunk_plan_kernel(ChunkArgs a) {

@@ -740,6 +740,10 @@ int chunk_plan(const sd_attn_shape *sh, ChunkPlan *p) {
   // 173 and 212).  Beside the halves their time is that of a workgroup's rows, more of them at once the more heads there
   // are (8 kv heads: 48 rows of 16 sequences at 500 keys 32 and 22, of 4 19.5 and 17.1, of one 16.4 and 16.8; at
   // 1000 keys of 16 41 and 35, of 4 25 and 24, of one 19 and 23; 16 rows of 16 at 500 16.9 and 16.3, of 8 at 1000 16 and 20).
+  // The lines are drawn at head_dim 128; at 64 they stand alike (block and chunk: 64 rows of 32 at 8192 233 and 190, of 4 at
+  // 32768 128 and 98, of one at 4096 20 and 31; single rows of 32 at 8192 96 and 128; 48 rows of 16 at 500 20 and 13).  They
+  // are on the wrong side for 64 rows of 4 sequences at 32768 keys with 2 kv heads (65 and 87; at head_dim 64 51 and 68) and
+  // for 16 rows of 16 at 500 with 8 (16.8 and 13.9; 13.5 and 9.8).
   const long long packed = (long long)G * sh->max_block;
   p->block = sh->max_block <= 64 && packed <= 256 && (packed <= 128 || groups * longest < 200000) &&
              !(p->halves && packed * (64 + groups) >= 10000 + 460 * steps);
